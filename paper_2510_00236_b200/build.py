@@ -8,31 +8,48 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc")
 LIB = os.path.join(CSRC, "libpestats.so")
-SOURCES = ["pe_api.cu"]
-HEADERS = ["pe_layout.cuh", "pe_optim.cuh", "pe_stage.cuh", "pe_short.cuh", "pe_simt.cuh", "pe_tc.cuh", "pe_tok.cuh", "pe_sm100.cuh", "../../include/pestats.h"]
+_COMMON = ["pe_host.cuh", "pe_sm100.cuh", "../../include/pestats.h"]
+# each source and the headers it includes
+SOURCES = {
+    "pe_api.cu": _COMMON + ["pe_layout.cuh", "pe_optim.cuh", "pe_stage.cuh", "pe_short.cuh", "pe_simt.cuh", "pe_tc.cuh", "pe_tok.cuh"],
+}
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
+def _stale(target: str, files) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+    t = os.path.getmtime(target)
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in files)
+
+
+def _object(source: str) -> str:
+    return os.path.join(CSRC, source.replace(".cu", ".o"))
+
+
+def _replacing(cmd, target):
+    """Runs cmd with its output in a file of its own that then takes the target's place."""
+    tmp = target + f".tmp{os.getpid()}"
+    subprocess.check_call(cmd + ["-o", tmp])
+    os.replace(tmp, target)
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
+    if not force and not any(_stale(LIB, [source] + headers) for source, headers in SOURCES.items()):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-           "-Xcompiler", "-fPIC", "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    flags = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
+
+    def compile_one(source):
+        if force or _stale(_object(source), [source] + SOURCES[source]):
+            _replacing(flags + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, source)], _object(source))
+
+    with ThreadPoolExecutor() as pool:
+        list(pool.map(compile_one, SOURCES))
+    _replacing(flags + ["-shared"] + [_object(source) for source in SOURCES], LIB)
     return LIB
 
 

@@ -15,6 +15,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/pestats.h"
+#include "pe_host.cuh"
 #include "pe_layout.cuh"
 #include "pe_optim.cuh"
 #include "pe_stage.cuh"
@@ -29,7 +30,7 @@ __device__ unsigned int g_dev_status = 0;   // first device-side wait that gave 
 
 static std::atomic<int> g_path{PE_PATH_AUTO};
 static std::atomic<int> g_last_path{PE_PATH_AUTO};
-static std::atomic<long long> g_launches{0};
+std::atomic<long long> g_launches{0};
 static std::atomic<int> g_fused_mode{PE_FUSED_AUTO};
 // Both outputs of a layer whose d_in fills neither 192- nor 128-column tiles well: from this sequence length on the running sum
 // of G_b may live in tensor memory beside a 256-column accumulator.
@@ -39,23 +40,11 @@ constexpr int PHI_UNSCALE = 4;      // internal phi of the staged per-token stat
 constexpr int PHI_CLIP_SCALE = 3;   // internal phi of the clipped sum: c_b * G_b (not part of pe_phi_t)
 constexpr int TC_BAND = 8;          // pair rows per band of the tile order (8 x 256 rows of d_out)
 
-constexpr int MAX_DEVICES = 64;
-struct DeviceInfo {
-  std::atomic<int> state{0};     // 0 unknown, 1 ready, -1 failed
-  int cc_major = 0, sm_count = 0;
-  unsigned int* status_ptr = nullptr;
-  bool tc_attr_set[64] = {};
-  bool tok_attr_set = false;
-};
 static DeviceInfo g_dev[MAX_DEVICES];
-static std::mutex g_dev_mutex;      // guards the lazily filled per-device state (first calls from several host threads)
-
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+std::mutex g_dev_mutex;
 static std::atomic<EncodeTiledFn> g_encode{nullptr};
 
-static pe_status_t device_info(DeviceInfo** out) {
+pe_status_t device_info(DeviceInfo** out) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) { cudaGetLastError(); return PE_ERR_CUDA; }
   DeviceInfo& d = g_dev[dev];
@@ -81,7 +70,7 @@ static pe_status_t device_info(DeviceInfo** out) {
   return d.cc_major == 10 ? PE_OK : PE_ERR_ARCH;
 }
 
-static EncodeTiledFn encode_fn() {
+EncodeTiledFn encode_fn() {
   EncodeTiledFn f = g_encode.load();
   if (f) return f;
   void* sym = nullptr;
@@ -94,15 +83,6 @@ static EncodeTiledFn encode_fn() {
   f = reinterpret_cast<EncodeTiledFn>(sym);
   g_encode.store(f);
   return f;
-}
-
-static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-static pe_status_t check_launch() {
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return PE_ERR_CUDA;
-  g_launches.fetch_add(1);
-  return PE_OK;
 }
 
 // [B, T, d] row-major (bf16, or fp32 read as tf32) viewed as a 3-D tensor (d, T, B); one box = 128
@@ -301,19 +281,6 @@ static pe_status_t zero_outputs(float* a, float* b, size_t bytes, cudaStream_t s
   return PE_OK;
 }
 
-// Launches `kernel` as a programmatic dependent of the kernel before it in the stream (every kernel launched this way waits for
-// that one to complete before it touches what others may have written: griddep_wait).
-template <typename Kernel, typename... Args>
-static pe_status_t launch_dependent(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t st, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr; cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-  return check_launch();
-}
 // Zeroes up to three [d_out, d_in] outputs with a kernel that lets its successor start when everything older has completed: the successor's
 // blocks follow on each SM as the zeroing block leaves it.  A programmatic dependent itself: against ordinary launches 1024 x 32 x 1024^2, both outputs,
 // 113 -> 110, 64 x 32 x 256 x 4096 18.6 -> 16.2 us (25 layers with MicroAdam 1597 -> 1576, which is within the runs' spread).  early: the successor starts at once and has to wait for it before anything else (what came
@@ -1024,7 +991,6 @@ static pe_status_t linear_stats_impl(const TIn* X, const TIn* dY, int B, int T, 
   return launch_simt<TIn, MODE_STATS>(di, X, dY, B, T, d_in, d_out, (int)phi, out_mean, out_stat, st, accumulate);
 }
 
-static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Constants of one Adam-family step (Algorithm 1): the scales that turn the sums into averages, the
 // bias corrections of step t, and the factor 1 / (1 - 1/B) of Eq. (6).
