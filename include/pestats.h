@@ -299,6 +299,56 @@ pe_status_t pe_token_sqstats_static(const void* X, const void* dY, int B, int T,
                                     float* out_stat, pe_stream_t stream);
 
 /*
+ * Normalisation layers.  For a row x of d features, mu = mean(x) and var = mean((x - mu)^2) for PE_NORM_LAYER, mu = 0 for
+ * PE_NORM_RMS (var is then the mean square):
+ *     rstd = 1 / sqrt(var + eps),   xh = (x - mu) * rstd,   y = xh * gain + bias.
+ * (The paper leaves such parameters to its general per-example form, which needs their gradient per example; Appendix E.2.2's
+ * transformer normalises before every block.)
+ * x, y: bf16 [rows, d], 16-byte aligned, not overlapping; gain, bias: fp32 [d], 4-byte aligned, NULL for ones / zeros; mean, rstd: fp32 [rows], 4-byte
+ * aligned, what pe_norm_backward reads; NULL to skip (PE_NORM_RMS writes no mean).  rows >= 0, d >= 1, rows * d < 2^40, eps >= 0.
+ * Sums are fp32: the mean first, then the squared deviations from it.  y is rounded once.  An unknown kind is PE_ERR_PHI.
+ */
+typedef enum { PE_NORM_LAYER = 0, PE_NORM_RMS = 1 } pe_norm_t;
+pe_status_t pe_norm_forward(const void* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind,
+                            float eps, void* y, float* mean, float* rstd, pe_stream_t stream);
+/* Same for fp32 x and y (4-byte aligned suffices). */
+pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind,
+                                float eps, float* y, float* mean, float* rstd, pe_stream_t stream);
+
+/*
+ * Its backward pass, with the statistics of the per-example gradients of gain and bias (Eq. (2) for these parameters).  With
+ * w = dy * gain,
+ *     dx = rstd * (w - xh * mean(w * xh) - mean(w))        (PE_NORM_RMS: without the last term)
+ *     G_b = sum_{t<T} dy[b,t] * xh[b,t],   H_b = sum_{t<T} dy[b,t]            (vectors of d)
+ *     gain_sum = sum_b G_b,  gain_stat = sum_b phi(G_b),  bias_sum = sum_b H_b,  bias_stat = sum_b phi(H_b).
+ * x, dy, dx: bf16 [B, T, d], 16-byte aligned; mean (PE_NORM_LAYER only), rstd: fp32 [B, T], what the forward pass wrote; gain as
+ * there.  Outputs: fp32 [d], 4-byte aligned, overwritten, or added to where accumulate != 0 (micro-batches); any of dx and the
+ * four may be NULL to skip it (not all).  dx must not overlap x or dy.
+ * workspace: device memory, 256-byte aligned, pe_norm_backward_workspace_bytes(B * T, d) bytes, contents undefined afterwards.
+ * B == 0 or T == 0 leaves dx alone and writes zeros (accumulate: nothing).  The sums' order depends on the sizes and the device
+ * alone: results repeat bit for bit.  An unknown kind or phi is PE_ERR_PHI.
+ */
+pe_status_t pe_norm_backward(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd, int B,
+                             int T, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, void* dx, float* gain_sum,
+                             float* gain_stat, float* bias_sum, float* bias_stat, void* workspace, size_t workspace_bytes,
+                             pe_stream_t stream);
+/* Same for fp32 x, dy and dx (4-byte aligned suffices). */
+pe_status_t pe_norm_backward_f32(const float* x, const float* dy, const float* gain, const float* mean, const float* rstd, int B,
+                                 int T, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, float* dx, float* gain_sum,
+                                 float* gain_stat, float* bias_sum, float* bias_stat, void* workspace, size_t workspace_bytes,
+                                 pe_stream_t stream);
+/* Same for a packed batch: x, dy, dx [total_rows, d], mean, rstd [total_rows], example b owns rows seq_offsets[b] ..
+ * seq_offsets[b+1]-1 as for pe_linear_stats_ragged (device array, same rules; an empty sequence contributes phi(0) = 0).  Rows of dx
+ * before the first and behind the last sequence are left as they were, and x and dy are not read there.
+ * workspace: pe_norm_backward_workspace_bytes(total_rows, d) bytes. */
+pe_status_t pe_norm_backward_ragged(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd,
+                                    const int* seq_offsets, int B, long long total_rows, int d, pe_norm_t kind, pe_phi_t phi,
+                                    int accumulate, void* dx, float* gain_sum, float* gain_stat, float* bias_sum,
+                                    float* bias_stat, void* workspace, size_t workspace_bytes, pe_stream_t stream);
+/* Bytes of workspace the backward calls need (0 for sizes out of range, and for no rows). */
+size_t pe_norm_backward_workspace_bytes(long long rows, int d);
+
+/*
  * One MicroAdam step over n parameters (Algorithm 1, MicroAdam branch; Eq. (3)):
  *     mu = s*sum_g/B;  nu = s^2*sum_g2/B;   m = beta1*m + (1-beta1)*mu;   v = beta2*v + (1-beta2)*nu
  *     mh = m/(1-beta1^step);  vh = v/(1-beta2^step)

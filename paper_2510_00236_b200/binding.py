@@ -22,6 +22,7 @@ __all__ = [
     "pe_linear_microadam_step", "pe_linear_microadam_step_f32", "pe_linear_microsignsgd_step", "pe_linear_fused_workspace_bytes",
     "pe_token_sqstats_fp8", "pe_token_sqstats_fp8_workspace_bytes", "pe_set_wait_limit_cycles", "pe_tile_order_band", "pe_plan_query", "PLAN_SHORT", "PLAN_SIMT_STATS", "PLAN_SIMT_TOKEN", "PLAN_SIMT_NORMS", "PLAN_TOKEN", "PLAN_NORMS",
     "pe_linear_stats_padded", "pe_linear_stats_padded_workspace_bytes", "pe_linear_stats_padded_workspace_bytes_for", "pe_conv2d_stats", "pe_conv2d_stats_workspace_bytes",
+    "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged", "pe_norm_backward_workspace_bytes", "NORM_LAYER", "NORM_RMS",
     "pe_set_fused_update", "FUSED_AUTO", "FUSED_ALWAYS", "FUSED_NEVER",
 ]
 
@@ -29,6 +30,8 @@ PHI_IDENTITY, PHI_SQUARE, PHI_SIGN = 0, 1, 2
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_TENSOR_NARROW, PATH_TENSOR_WIDE = 0, 1, 2, 3, 4
 FUSED_AUTO, FUSED_ALWAYS, FUSED_NEVER = 0, 1, 2      # pe_fused_mode_t
 PLAN_SHORT, PLAN_SIMT_STATS, PLAN_SIMT_TOKEN, PLAN_SIMT_NORMS, PLAN_TOKEN, PLAN_NORMS = range(6)      # pe_plan_t
+NORM_LAYER, NORM_RMS = 0, 1      # pe_norm_t
+_NORM_NAMES = {"layer": NORM_LAYER, "rms": NORM_RMS}
 _PHI_NAMES = {"identity": PHI_IDENTITY, "square": PHI_SQUARE, "sign": PHI_SIGN}
 
 # every symbol include/pestats.h declares
@@ -42,6 +45,7 @@ EXPORTED_SYMBOLS = [
     "pe_token_sqstats_fp8", "pe_token_sqstats_fp8_workspace_bytes", "pe_set_wait_limit_cycles", "pe_tile_order_band", "pe_plan_query",
     "pe_set_fused_update", "pe_linear_stats_padded", "pe_linear_stats_padded_workspace_bytes", "pe_linear_stats_padded_workspace_bytes_for", "pe_conv2d_stats",
     "pe_conv2d_stats_workspace_bytes",
+    "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged", "pe_norm_backward_workspace_bytes",
 ]
 ADAM_VARIANTS = {"adam": 0, "microadam": 1, "microadam_var": 2, "microadam_msq": 3}      # pe_adam_variant_t
 STATIC_SCRATCH_BYTES = 32 * 1024 * 1024      # PE_STATIC_SCRATCH_BYTES of pestats.h
@@ -104,6 +108,13 @@ def load_library() -> ctypes.CDLL:
     lib.pe_token_sqstats_static.argtypes = [vp, vp, i, i, i, i, vp, vp]
     lib.pe_token_sqstats_staged_workspace_bytes.argtypes = [i, i, i, i]
     lib.pe_token_sqstats_staged_workspace_bytes.restype = sz
+    for name in ("pe_norm_forward", "pe_norm_forward_f32"):
+        getattr(lib, name).argtypes = [vp, vp, vp, ll, i, i, f, vp, vp, vp, vp]
+    for name in ("pe_norm_backward", "pe_norm_backward_f32"):
+        getattr(lib, name).argtypes = [vp] * 5 + [i] * 6 + [vp] * 6 + [sz, vp]
+    lib.pe_norm_backward_ragged.argtypes = [vp] * 6 + [i, ll, i, i, i, i] + [vp] * 6 + [sz, vp]
+    lib.pe_norm_backward_workspace_bytes.argtypes = [ll, i]
+    lib.pe_norm_backward_workspace_bytes.restype = sz
     lib.microadam_step.argtypes = [vp, vp, vp, vp, vp, vp, ll, i, f, f, f, f, f, i, f, i, vp]
     lib.microadam_family_step.argtypes = [vp, vp, vp, vp, vp, vp, ll, i, i, f, f, f, f, f, i, f, i, vp]
     lib.microsignsgd_step.argtypes = [vp, vp, vp, vp, ll, i, f, f, f, vp]
@@ -128,6 +139,7 @@ def load_library() -> ctypes.CDLL:
                  "pe_token_sqstats_staged", "pe_token_sqstats_fp8",
                  "pe_linear_stats_ragged", "pe_example_sqnorms_ragged", "pe_linear_clipped_sum",
                  "pe_linear_microadam_step", "pe_linear_microadam_step_f32", "pe_linear_microsignsgd_step",
+                 "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged",
                  "microadam_step", "microadam_family_step", "microsignsgd_step", "pe_get_async_status", "pe_set_path", "pe_last_path"):
         getattr(lib, name).restype = i
     _lib = lib
@@ -528,6 +540,121 @@ def pe_token_sqstats_f32(X, dY, out_stat=None):
     _out_check("out_stat", out_stat, d_out, d_in)
     _launch("pe_token_sqstats_f32", X, X.data_ptr(), dY.data_ptr(), B, T, d_in, d_out, out_stat.data_ptr())
     return out_stat
+
+
+def _norm_kind(kind) -> int:
+    return _NORM_NAMES[kind] if isinstance(kind, str) else int(kind)
+
+
+def _float_rows(name, t, shape, device):
+    if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != device):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on the inputs' device")
+
+
+def _norm_input(name, t, shape=None, dtype=None, device=None):
+    """Rows of d features (the last dimension), contiguous, bfloat16 or float32."""
+    if t.dtype not in (torch.bfloat16, torch.float32) or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, all of them the same")
+    if t.dim() < 1 or not t.is_contiguous() or (shape is not None and t.shape != shape) or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be contiguous, of x's shape and on its device")
+
+
+def pe_norm_forward(x, gain=None, bias=None, *, kind="layer", eps=1e-5, out=None, mean=None, rstd=None):
+    """y = (x - mean) * rstd * gain + bias over the last dimension of x (bf16 or float32, contiguous); kind "layer" or "rms" (mean = 0).
+    gain, bias: float32 [d] or None.  Returns (y, mean, rstd); mean and rstd, float32 of x's leading shape, are what pe_norm_backward reads
+    (mean is None for "rms").  Missing outputs are allocated."""
+    _norm_input("x", x)
+    lead, d, code = x.shape[:-1], x.shape[-1], _norm_kind(kind)
+    _float_rows("gain", gain, (d,), x.device)
+    _float_rows("bias", bias, (d,), x.device)
+    if out is None:
+        out = torch.empty_like(x)
+    _norm_input("out", out, x.shape, x.dtype, x.device)
+    if rstd is None:
+        rstd = x.new_empty(lead, dtype=torch.float32)
+    if code == NORM_RMS:
+        mean = None
+    elif mean is None:
+        mean = x.new_empty(lead, dtype=torch.float32)
+    _float_rows("mean", mean, lead, x.device)
+    _float_rows("rstd", rstd, lead, x.device)
+    _launch("pe_norm_forward" if x.dtype == torch.bfloat16 else "pe_norm_forward_f32", x, x.data_ptr(), _ptr(gain), _ptr(bias), x.numel() // d if d else 0, d,
+            code, float(eps), out.data_ptr(), _ptr(mean), rstd.data_ptr())
+    return out, mean, rstd
+
+
+def pe_norm_forward_f32(x, gain=None, bias=None, **kw):
+    """pe_norm_forward for float32 x (the C entry point of the same name)."""
+    if x.dtype != torch.float32:
+        raise TypeError("x must be torch.float32")
+    return pe_norm_forward(x, gain, bias, **kw)
+
+
+def pe_norm_backward_workspace_bytes(rows, d) -> int:
+    return (_lib or load_library()).pe_norm_backward_workspace_bytes(rows, d)
+
+
+def _norm_backward(x, dy, gain, mean, rstd, seq_offsets, phi, kind, dx, gain_sum, gain_stat, bias_sum, bias_stat, accumulate, workspace):
+    _norm_input("x", x)
+    _norm_input("dy", dy, x.shape, x.dtype, x.device)
+    code, d, lead = _norm_kind(kind), x.shape[-1], x.shape[:-1]
+    if dx is None:
+        dx = torch.empty_like(x) if seq_offsets is None else torch.zeros_like(x)      # rows of no sequence: the library leaves them alone
+    _norm_input("dx", dx, x.shape, x.dtype, x.device)
+    if x.numel() and dx.data_ptr() in (x.data_ptr(), dy.data_ptr()):
+        raise ValueError("dx must not overlap x or dy")
+    _float_rows("gain", gain, (d,), x.device)
+    if code == NORM_RMS:
+        mean = None
+    elif mean is None:
+        raise ValueError("mean is required for a layer norm")
+    _float_rows("mean", mean, lead, x.device)
+    _float_rows("rstd", rstd, lead, x.device)
+    sums = [gain_sum, gain_stat, bias_sum, bias_stat]
+    if all(t is None for t in sums):
+        if accumulate:
+            raise ValueError("accumulate needs the sums to add to")
+        sums = [x.new_empty((d,), dtype=torch.float32) for _ in range(2 if code == NORM_RMS else 4)] + [None] * (2 if code == NORM_RMS else 0)
+    for name, t in zip(("gain_sum", "gain_stat", "bias_sum", "bias_stat"), sums):
+        _float_rows(name, t, (d,), x.device)
+    rows = rstd.numel()
+    if workspace is None:
+        workspace = x.new_empty((pe_norm_backward_workspace_bytes(rows, d),), dtype=torch.uint8)
+    elif workspace.device != x.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on x's device")
+    tail = (d, code, _phi(phi), int(bool(accumulate)), dx.data_ptr(), *map(_ptr, sums), workspace.data_ptr() or None, workspace.numel() * workspace.element_size())
+    head = (x.data_ptr(), dy.data_ptr(), _ptr(gain), _ptr(mean), rstd.data_ptr())
+    if seq_offsets is not None:
+        _launch("pe_norm_backward_ragged", x, *head, seq_offsets.data_ptr(), seq_offsets.numel() - 1, rows, *tail)
+    else:
+        _launch("pe_norm_backward" if x.dtype == torch.bfloat16 else "pe_norm_backward_f32", x, *head, x.shape[0], x.shape[1], *tail)
+    return (dx, *sums)
+
+
+def pe_norm_backward(x, dy, gain, mean, rstd, phi, *, kind="layer", dx=None, gain_sum=None, gain_stat=None, bias_sum=None, bias_stat=None,
+                     accumulate=False, workspace=None):
+    """Backward pass of pe_norm_forward over x, dy [B, T, d] (bf16 or float32), with the per-example gradients of gain and bias summed over the
+    examples as they are and through phi.  Returns (dx, gain_sum, gain_stat, bias_sum, bias_stat).  If none of the four sums is given all are
+    allocated (kind "rms": the gain's two); otherwise those left out are not computed and come back as None.  accumulate adds to the
+    given sums.  workspace: uint8 tensor of pe_norm_backward_workspace_bytes(B * T, d) bytes, allocated when omitted."""
+    if x.dim() != 3:
+        raise ValueError("x must be [B, T, d]")
+    return _norm_backward(x, dy, gain, mean, rstd, None, phi, kind, dx, gain_sum, gain_stat, bias_sum, bias_stat, accumulate, workspace)
+
+
+def pe_norm_backward_f32(x, dy, gain, mean, rstd, phi, **kw):
+    """pe_norm_backward for float32 inputs (the C entry point of the same name)."""
+    if x.dtype != torch.float32:
+        raise TypeError("x and dy must be torch.float32")
+    return pe_norm_backward(x, dy, gain, mean, rstd, phi, **kw)
+
+
+def pe_norm_backward_ragged(x, dy, gain, mean, rstd, seq_offsets, phi, *, kind="layer", dx=None, gain_sum=None, gain_stat=None, bias_sum=None,
+                            bias_stat=None, accumulate=False, workspace=None):
+    """pe_norm_backward for a packed batch (bf16): x, dy [rows, d], mean, rstd [rows], example b owns rows seq_offsets[b] ..
+    seq_offsets[b+1]-1 (int32 device tensor).  Rows of no sequence are left as they were in dx (zeros where it is allocated here)."""
+    _ragged_check(x, dy, seq_offsets)
+    return _norm_backward(x, dy, gain, mean, rstd, seq_offsets, phi, kind, dx, gain_sum, gain_stat, bias_sum, bias_stat, accumulate, workspace)
 
 
 def _flat_f32(name, t, n=None):

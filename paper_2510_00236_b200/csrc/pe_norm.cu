@@ -1,0 +1,228 @@
+// Entry points of the normalisation layers: argument checks, the choice of the launch, and the launches.
+#include <algorithm>
+
+#include "pe_host.cuh"
+#include "pe_norm.cuh"
+
+namespace pe {
+
+// ---------------------------------------------------------------- forward
+struct ForwardPlan {
+  int G, nv, threads;      // threads per row, vectors per thread, threads per block; G = 0: the kernel for rows of any width
+};
+// A power of two of lanes per row while one vector each covers it, then a warp with up to 8 vectors each, then several warps.
+static ForwardPlan plan_forward(int d, int E) {
+  const int vectors = (d + E - 1) / E;
+  ForwardPlan p = {32, 1, 256};
+  if (vectors <= 32) {
+    p.G = 1;
+    while (p.G < vectors) p.G *= 2;
+  } else if (vectors <= 256) {
+    while (p.nv * 32 < vectors) p.nv *= 2;
+  } else if (vectors <= 8192) {
+    p.nv = 8;
+    p.G = (vectors + 255) / 256 * 32;
+  } else {
+    p.G = 0;
+    p.threads = 1024;
+    return p;
+  }
+  p.threads = p.G * std::max(1, 256 / p.G);
+  return p;
+}
+
+template <typename T, int E, bool RMS>
+static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain, const float* bias, long long rows, int d, float eps, T* y,
+                                  float* mean, float* rstd, cudaStream_t st) {
+  const ForwardPlan p = plan_forward(d, E);
+  if (p.G == 0)
+    return launch_dependent(norm_forward_wide_kernel<T, RMS>, dim3((unsigned)std::min<long long>(rows, 2ll * di->sm_count)), p.threads, 0, st, x, gain,
+                            bias, rows, d, eps, y, mean, rstd);
+  const int groups = p.threads / p.G;
+  const long long blocks = (rows + groups - 1) / groups;
+  const dim3 grid((unsigned)std::min<long long>(blocks, 1 << 30));
+  switch (p.nv) {
+    case 1: return launch_dependent(norm_forward_kernel<T, E, 1, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
+    case 2: return launch_dependent(norm_forward_kernel<T, E, 2, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
+    case 4: return launch_dependent(norm_forward_kernel<T, E, 4, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
+    default: return launch_dependent(norm_forward_kernel<T, E, 8, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
+  }
+}
+
+static bool norm_size_ok(long long rows, int d) { return rows >= 0 && d >= 1 && rows < (1ll << 40) && (rows == 0 || rows <= ((1ll << 40) - 1) / d); }
+static bool kind_ok(pe_norm_t kind) { return kind == PE_NORM_LAYER || kind == PE_NORM_RMS; }
+
+template <typename T>
+static pe_status_t forward_impl(const T* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind, float eps, T* y, float* mean,
+                                float* rstd, cudaStream_t st) {
+  if (!norm_size_ok(rows, d) || !(eps >= 0.f)) return PE_ERR_DIM;
+  if (!kind_ok(kind)) return PE_ERR_PHI;
+  if (rows > 0 && (!x || !y)) return PE_ERR_NULL;
+  const size_t al = sizeof(T) == 2 ? 16 : 4;
+  if (!aligned(x, al) || !aligned(y, al) || !aligned(gain, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return PE_ERR_ALIGN;
+  DeviceInfo* di = nullptr;
+  const pe_status_t rc = device_info(&di);
+  if (rc != PE_OK) return rc;
+  if (rows == 0) return PE_OK;
+  constexpr int E = 16 / (int)sizeof(T);
+  const bool rms = kind == PE_NORM_RMS;
+  if (d % E == 0 && aligned(x, 16) && aligned(y, 16))
+    return rms ? launch_forward<T, E, true>(di, x, gain, bias, rows, d, eps, y, mean, rstd, st)
+               : launch_forward<T, E, false>(di, x, gain, bias, rows, d, eps, y, mean, rstd, st);
+  return rms ? launch_forward<T, 1, true>(di, x, gain, bias, rows, d, eps, y, mean, rstd, st)
+             : launch_forward<T, 1, false>(di, x, gain, bias, rows, d, eps, y, mean, rstd, st);
+}
+
+// ---------------------------------------------------------------- backward
+constexpr int NORM_WHOLE_THREADS = 512;      // a block of the one-pass kernel: rows of up to 4096 features
+constexpr int NORM_SLAB_THREADS = 256;       // a block of the two-pass kernel: 2048 features
+constexpr int NORM_SM_COUNT = 148;           // the workspace is sized for launches of at most this many SMs
+struct BackwardPlan {
+  bool whole;
+  int G, groups, blocks, slabs;              // blocks along the rows; slabs of features (two-pass)
+  size_t ends_at, means_at, bytes;           // workspace: elements, their flags, the rows' means
+};
+static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count) {
+  BackwardPlan p = {};
+  sm_count = std::min(sm_count, NORM_SM_COUNT);
+  const int threads = (d + NORM_COLS - 1) / NORM_COLS;
+  p.whole = threads <= NORM_WHOLE_THREADS;
+  p.slabs = 1;
+  if (!p.whole) {
+    p.G = NORM_SLAB_THREADS;
+    p.slabs = (threads + p.G - 1) / p.G;
+  } else if (threads <= 32) {
+    p.G = 1;
+    while (p.G < threads) p.G *= 2;
+  } else {
+    p.G = (threads + 31) / 32 * 32;
+  }
+  p.groups = std::max(1, 256 / p.G);
+  const long long want = std::max(1ll, rows / (8ll * p.groups));      // at least eight rows to a worker
+  const long long most = p.whole ? sm_count * std::max(1, 512 / (p.G * p.groups)) : std::max(1, 2 * sm_count / p.slabs);
+  p.blocks = (int)std::min(want, most);
+  p.ends_at = align_up((size_t)p.blocks * NORM_PARTS * kinds * d * sizeof(float), 256);
+  p.means_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
+  p.bytes = p.means_at + (p.whole ? 0 : align_up((size_t)rows * sizeof(float2), 256));
+  return p;
+}
+
+template <typename T, int E, bool RMS, int KINDS>
+static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, const BackwardPlan& p, char* ws, cudaStream_t st) {
+  const int threads = p.G * p.groups;
+  const int smem = (int)(((size_t)threads * NORM_PARTS * NORM_COLS) * sizeof(float) + p.groups * sizeof(int));
+  a.G = p.G;
+  a.parts = reinterpret_cast<float*>(ws);
+  a.ends = reinterpret_cast<int*>(ws + p.ends_at);
+  a.row_means = reinterpret_cast<const float2*>(ws + p.means_at);
+  auto large_smem = [&](auto kernel) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess ? PE_OK : (cudaGetLastError(), PE_ERR_CUDA);
+  };
+  if (p.whole) {
+    auto kernel = norm_backward_kernel<T, E, RMS, KINDS, true, NORM_WHOLE_THREADS>;
+    if (smem > 48 * 1024) {
+      const pe_status_t rc = large_smem(kernel);
+      if (rc != PE_OK) return rc;
+    }
+    return launch_dependent(kernel, dim3(p.blocks), threads, smem, st, x, dy, dx, a);
+  }
+  const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
+                                          a, reinterpret_cast<float2*>(ws + p.means_at));
+  if (rc != PE_OK) return rc;
+  return launch_dependent(norm_backward_kernel<T, E, RMS, KINDS, false, NORM_SLAB_THREADS>, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
+}
+
+template <typename T>
+static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, const float* mean, const float* rstd, const int* offsets, bool packed, int B,
+                                 int T_, long long rows, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, T* dx, float* gain_sum, float* gain_stat,
+                                 float* bias_sum, float* bias_stat, void* workspace, size_t workspace_bytes, cudaStream_t st) {
+  if (B < 0 || T_ < 0 || !norm_size_ok(rows, d) || (packed && rows >= (1ll << 31))) return PE_ERR_DIM;
+  if (!kind_ok(kind) || (phi != PE_PHI_IDENTITY && phi != PE_PHI_SQUARE && phi != PE_PHI_SIGN)) return PE_ERR_PHI;
+  const bool empty = B == 0 || rows == 0;
+  if (!empty && (!x || !dy || !rstd || (kind == PE_NORM_LAYER && !mean) || (packed && !offsets))) return PE_ERR_NULL;
+  if (!dx && !gain_sum && !gain_stat && !bias_sum && !bias_stat) return PE_ERR_NULL;
+  const size_t al = sizeof(T) == 2 ? 16 : 4;
+  if (!aligned(x, al) || !aligned(dy, al) || !aligned(dx, al)) return PE_ERR_ALIGN;
+  for (const void* q : {(const void*)gain, (const void*)mean, (const void*)rstd, (const void*)offsets, (const void*)gain_sum, (const void*)gain_stat,
+                        (const void*)bias_sum, (const void*)bias_stat})
+    if (!aligned(q, 4)) return PE_ERR_ALIGN;
+  DeviceInfo* di = nullptr;
+  pe_status_t rc = device_info(&di);
+  if (rc != PE_OK) return rc;
+  if (empty) {
+    if (!accumulate)
+      for (float* q : {gain_sum, gain_stat, bias_sum, bias_stat})
+        if (q && cudaMemsetAsync(q, 0, (size_t)d * sizeof(float), st) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    return PE_OK;
+  }
+  const bool bias = bias_sum || bias_stat, rms = kind == PE_NORM_RMS;
+  const int kinds = bias ? 2 : 1;
+  const BackwardPlan p = plan_backward(rows, d, kinds, di->sm_count);
+  if (!workspace || workspace_bytes < p.bytes) return PE_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return PE_ERR_ALIGN;
+  NormBackward a = {};
+  a.gain = gain; a.mean = mean; a.rstd = rstd; a.offsets = packed ? offsets : nullptr;
+  a.rows = rows; a.B = B; a.T = T_; a.d = d; a.phi = (int)phi;
+  constexpr int E = 16 / (int)sizeof(T);
+  char* ws = static_cast<char*>(workspace);
+  const bool vec = d % E == 0 && aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16);
+  auto with = [&](auto e) {
+    constexpr int EE = decltype(e)::value;
+    if (rms) return bias ? launch_backward<T, EE, true, 2>(di, x, dy, dx, a, p, ws, st) : launch_backward<T, EE, true, 1>(di, x, dy, dx, a, p, ws, st);
+    return bias ? launch_backward<T, EE, false, 2>(di, x, dy, dx, a, p, ws, st) : launch_backward<T, EE, false, 1>(di, x, dy, dx, a, p, ws, st);
+  };
+  rc = vec ? with(std::integral_constant<int, E>{}) : with(std::integral_constant<int, 1>{});
+  if (rc != PE_OK || (!bias && !gain_sum && !gain_stat)) return rc;
+  const float* parts = reinterpret_cast<const float*>(ws);
+  const int* ends = reinterpret_cast<const int*>(ws + p.ends_at);
+  const dim3 grid((unsigned)(kinds * ((d + 31) / 32)));
+  if (bias)
+    return launch_dependent(norm_join_kernel<2>, grid, 32 * NORM_JOIN_WARPS, 0, st, parts, ends, p.blocks, d, (int)phi, accumulate, gain_sum, gain_stat,
+                            bias_sum, bias_stat);
+  return launch_dependent(norm_join_kernel<1>, grid, 32 * NORM_JOIN_WARPS, 0, st, parts, ends, p.blocks, d, (int)phi, accumulate, gain_sum, gain_stat,
+                          bias_sum, bias_stat);
+}
+
+}  // namespace pe
+
+using namespace pe;
+
+extern "C" {
+
+pe_status_t pe_norm_forward(const void* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind, float eps, void* y, float* mean,
+                            float* rstd, pe_stream_t stream) {
+  return forward_impl(static_cast<const __nv_bfloat16*>(x), gain, bias, rows, d, kind, eps, static_cast<__nv_bfloat16*>(y), mean, rstd,
+                      reinterpret_cast<cudaStream_t>(stream));
+}
+pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind, float eps, float* y, float* mean,
+                                float* rstd, pe_stream_t stream) {
+  return forward_impl(x, gain, bias, rows, d, kind, eps, y, mean, rstd, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t pe_norm_backward_workspace_bytes(long long rows, int d) {
+  if (!norm_size_ok(rows, d) || rows == 0) return 0;
+  return plan_backward(rows, d, 2, NORM_SM_COUNT).bytes;
+}
+
+pe_status_t pe_norm_backward(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd, int B, int T, int d, pe_norm_t kind,
+                             pe_phi_t phi, int accumulate, void* dx, float* gain_sum, float* gain_stat, float* bias_sum, float* bias_stat, void* workspace,
+                             size_t workspace_bytes, pe_stream_t stream) {
+  return backward_impl(static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(dy), gain, mean, rstd, nullptr, false, B, T,
+                       (long long)B * T, d, kind, phi, accumulate, static_cast<__nv_bfloat16*>(dx), gain_sum, gain_stat, bias_sum, bias_stat, workspace,
+                       workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+pe_status_t pe_norm_backward_f32(const float* x, const float* dy, const float* gain, const float* mean, const float* rstd, int B, int T, int d,
+                                 pe_norm_t kind, pe_phi_t phi, int accumulate, float* dx, float* gain_sum, float* gain_stat, float* bias_sum,
+                                 float* bias_stat, void* workspace, size_t workspace_bytes, pe_stream_t stream) {
+  return backward_impl(x, dy, gain, mean, rstd, nullptr, false, B, T, (long long)B * T, d, kind, phi, accumulate, dx, gain_sum, gain_stat, bias_sum,
+                       bias_stat, workspace, workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+pe_status_t pe_norm_backward_ragged(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd, const int* seq_offsets, int B,
+                                    long long total_rows, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, void* dx, float* gain_sum,
+                                    float* gain_stat, float* bias_sum, float* bias_stat, void* workspace, size_t workspace_bytes, pe_stream_t stream) {
+  return backward_impl(static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(dy), gain, mean, rstd, seq_offsets, true, B, 1, total_rows, d,
+                       kind, phi, accumulate, static_cast<__nv_bfloat16*>(dx), gain_sum, gain_stat, bias_sum, bias_stat, workspace, workspace_bytes,
+                       reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
