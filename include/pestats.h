@@ -394,6 +394,40 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
                               pe_stream_t stream);
 
 /*
+ * Orthogonalised matrices: `steps` quintic Newton-Schulz steps on each of `count` matrices G [rows, cols],
+ *     X = G / ||G||_F,   then   X <- a X + (b A + c A A) X,  A = X X^T  (or, the same, X A with A = X^T X),
+ *     (a, b, c) = (3.4445, -4.7750, 2.0315):
+ * a s + b s^3 + c s^5 applied `steps` times to the singular values of X; five steps bring those above about 1/100 of ||G||_F to
+ * between 0.68 and 1.21, so that out is close to U V^T of G = U S V^T.  (The paper's statistics leave the mean gradient to elementwise updates; this
+ * is the update for whole matrices beside them.)  G = 0 gives 0; an infinity or NaN gives NaN in that matrix alone.
+ * G, out: bf16 [count, rows, cols], 16-byte aligned; out may be G.  count >= 0, rows, cols >= 1 (at most 2^30), count < 65536, count * rows * cols
+ * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
+ * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
+ * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 per entry of A),
+ * contents undefined afterwards.  Results repeat bit for bit.
+ */
+pe_status_t pe_orthogonalize(const void* G, int count, int rows, int cols, int steps, void* out, void* workspace,
+                             size_t workspace_bytes, pe_stream_t stream);
+/* Same for fp32 G and out (4-byte aligned suffices). */
+pe_status_t pe_orthogonalize_f32(const float* G, int count, int rows, int cols, int steps, float* out, void* workspace,
+                                 size_t workspace_bytes, pe_stream_t stream);
+/* Bytes of workspace pe_orthogonalize, pe_orthogonalize_f32 and muon_step need (0 for sizes out of range, and for no matrices). */
+size_t pe_orthogonalize_workspace_bytes(int count, int rows, int cols);
+
+/*
+ * One step with the orthogonalised momentum on `count` matrices of parameters [rows, cols], O the function above:
+ *     g = s*sum_g/B;   m = beta*m + (1-beta)*g;   U = nesterov ? (1-beta)*g + beta*m : m
+ *     theta = theta - lr*update_scale*O(U) - weight_decay*theta                  (decay not scaled by lr, as microadam_step)
+ * theta, m: fp32 [count, rows, cols], updated in place; sum_g: fp32, the out_mean of pe_linear_stats, s = grad_scale as for
+ * microadam_step; theta_lp: optional bf16 copy of the new theta.  All 16-byte aligned, none overlapping another.  O(U) does not depend on U's scale;
+ * update_scale is the caller's factor for it, often sqrt(max(1, rows / cols)).  Sizes, steps and workspace as for
+ * pe_orthogonalize.  After PE_ERR_TIMEOUT theta is left as it was (of the matrices not yet written), m has been updated.
+ */
+pe_status_t muon_step(float* theta, void* theta_lp, float* m, const float* sum_g, int count, int rows, int cols, int B,
+                      float grad_scale, float lr, float beta, int nesterov, int steps, float update_scale, float weight_decay,
+                      void* workspace, size_t workspace_bytes, pe_stream_t stream);
+
+/*
  * Statistics and parameter update in ONE launch (Algorithm 1 applied to the statistics of Eq. (2) where
  * they are formed: the thread block that holds, or completes, a tile's sums over the whole batch applies
  * the update to that tile of the parameters, so the sums need not be written out and read back and the

@@ -23,6 +23,7 @@ __all__ = [
     "pe_token_sqstats_fp8", "pe_token_sqstats_fp8_workspace_bytes", "pe_set_wait_limit_cycles", "pe_tile_order_band", "pe_plan_query", "PLAN_SHORT", "PLAN_SIMT_STATS", "PLAN_SIMT_TOKEN", "PLAN_SIMT_NORMS", "PLAN_TOKEN", "PLAN_NORMS",
     "pe_linear_stats_padded", "pe_linear_stats_padded_workspace_bytes", "pe_linear_stats_padded_workspace_bytes_for", "pe_conv2d_stats", "pe_conv2d_stats_workspace_bytes",
     "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged", "pe_norm_backward_workspace_bytes", "NORM_LAYER", "NORM_RMS",
+    "pe_orthogonalize", "pe_orthogonalize_f32", "pe_orthogonalize_workspace_bytes", "muon_step",
     "pe_set_fused_update", "FUSED_AUTO", "FUSED_ALWAYS", "FUSED_NEVER",
 ]
 
@@ -46,6 +47,7 @@ EXPORTED_SYMBOLS = [
     "pe_set_fused_update", "pe_linear_stats_padded", "pe_linear_stats_padded_workspace_bytes", "pe_linear_stats_padded_workspace_bytes_for", "pe_conv2d_stats",
     "pe_conv2d_stats_workspace_bytes",
     "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged", "pe_norm_backward_workspace_bytes",
+    "pe_orthogonalize", "pe_orthogonalize_f32", "pe_orthogonalize_workspace_bytes", "muon_step",
 ]
 ADAM_VARIANTS = {"adam": 0, "microadam": 1, "microadam_var": 2, "microadam_msq": 3}      # pe_adam_variant_t
 STATIC_SCRATCH_BYTES = 32 * 1024 * 1024      # PE_STATIC_SCRATCH_BYTES of pestats.h
@@ -115,6 +117,11 @@ def load_library() -> ctypes.CDLL:
     lib.pe_norm_backward_ragged.argtypes = [vp] * 6 + [i, ll, i, i, i, i] + [vp] * 6 + [sz, vp]
     lib.pe_norm_backward_workspace_bytes.argtypes = [ll, i]
     lib.pe_norm_backward_workspace_bytes.restype = sz
+    for name in ("pe_orthogonalize", "pe_orthogonalize_f32"):
+        getattr(lib, name).argtypes = [vp, i, i, i, i, vp, vp, sz, vp]
+    lib.pe_orthogonalize_workspace_bytes.argtypes = [i, i, i]
+    lib.pe_orthogonalize_workspace_bytes.restype = sz
+    lib.muon_step.argtypes = [vp] * 4 + [i] * 4 + [f] * 3 + [i, i, f, f, vp, sz, vp]
     lib.microadam_step.argtypes = [vp, vp, vp, vp, vp, vp, ll, i, f, f, f, f, f, i, f, i, vp]
     lib.microadam_family_step.argtypes = [vp, vp, vp, vp, vp, vp, ll, i, i, f, f, f, f, f, i, f, i, vp]
     lib.microsignsgd_step.argtypes = [vp, vp, vp, vp, ll, i, f, f, f, vp]
@@ -140,6 +147,7 @@ def load_library() -> ctypes.CDLL:
                  "pe_linear_stats_ragged", "pe_example_sqnorms_ragged", "pe_linear_clipped_sum",
                  "pe_linear_microadam_step", "pe_linear_microadam_step_f32", "pe_linear_microsignsgd_step",
                  "pe_norm_forward", "pe_norm_forward_f32", "pe_norm_backward", "pe_norm_backward_f32", "pe_norm_backward_ragged",
+                 "pe_orthogonalize", "pe_orthogonalize_f32", "muon_step",
                  "microadam_step", "microadam_family_step", "microsignsgd_step", "pe_get_async_status", "pe_set_path", "pe_last_path"):
         getattr(lib, name).restype = i
     _lib = lib
@@ -655,6 +663,64 @@ def pe_norm_backward_ragged(x, dy, gain, mean, rstd, seq_offsets, phi, *, kind="
     seq_offsets[b+1]-1 (int32 device tensor).  Rows of no sequence are left as they were in dx (zeros where it is allocated here)."""
     _ragged_check(x, dy, seq_offsets)
     return _norm_backward(x, dy, gain, mean, rstd, seq_offsets, phi, kind, dx, gain_sum, gain_stat, bias_sum, bias_stat, accumulate, workspace)
+
+
+def pe_orthogonalize_workspace_bytes(count, rows, cols) -> int:
+    return (_lib or load_library()).pe_orthogonalize_workspace_bytes(count, rows, cols)
+
+
+def _matrices(name, t, dtypes, shape=None, device=None):
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}")
+    if t.dim() not in (2, 3) or not t.is_contiguous() or (shape is not None and t.shape != shape) or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a contiguous [rows, cols] or [count, rows, cols] tensor, all of one shape and device")
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def _ns_workspace(workspace, like, count, rows, cols):
+    if workspace is None:
+        workspace = like.new_empty((pe_orthogonalize_workspace_bytes(count, rows, cols),), dtype=torch.uint8)
+    elif workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the matrices' device")
+    return workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
+
+
+def pe_orthogonalize(G, steps=5, out=None, workspace=None):
+    """`steps` quintic Newton-Schulz steps on each matrix of G ([rows, cols] or [count, rows, cols], bf16 or float32) divided by its Frobenius
+    norm; close to U V^T of G = U S V^T.  out (G's type and shape; may be G) is allocated when omitted, like workspace, a uint8 tensor of
+    pe_orthogonalize_workspace_bytes(count, rows, cols) bytes."""
+    count, rows, cols = _matrices("G", G, (torch.bfloat16, torch.float32))
+    if out is None:
+        out = torch.empty_like(G)
+    _matrices("out", out, (G.dtype,), G.shape, G.device)
+    ws, ws_bytes = _ns_workspace(workspace, G, count, rows, cols)
+    _launch("pe_orthogonalize" if G.dtype == torch.bfloat16 else "pe_orthogonalize_f32", G, G.data_ptr(), count, rows, cols, int(steps), out.data_ptr(), ws,
+            ws_bytes)
+    return out
+
+
+def pe_orthogonalize_f32(G, steps=5, out=None, workspace=None):
+    """pe_orthogonalize for float32 matrices (the C entry point of the same name)."""
+    if G.dtype != torch.float32:
+        raise TypeError("G must be torch.float32")
+    return pe_orthogonalize(G, steps, out, workspace)
+
+
+def muon_step(theta, m, sum_g, B, *, lr, beta, steps=5, nesterov=True, update_scale=None, grad_scale=1.0, weight_decay=0.0, theta_lp=None,
+              workspace=None):
+    """In-place update of (theta, m), float32 [rows, cols] or [count, rows, cols], by the orthogonalised momentum of sum_b G_b.
+    update_scale defaults to sqrt(max(1, rows / cols)); workspace as for pe_orthogonalize."""
+    count, rows, cols = _matrices("theta", theta, (torch.float32,))
+    for name, t in (("m", m), ("sum_g", sum_g)):
+        _matrices(name, t, (torch.float32,), theta.shape, theta.device)
+    if theta_lp is not None:
+        _matrices("theta_lp", theta_lp, (torch.bfloat16,), theta.shape, theta.device)
+    if update_scale is None:
+        update_scale = max(1.0, rows / cols) ** 0.5 if cols else 1.0
+    ws, ws_bytes = _ns_workspace(workspace, theta, count, rows, cols)
+    _launch("muon_step", theta, theta.data_ptr(), _ptr(theta_lp), m.data_ptr(), sum_g.data_ptr(), count, rows, cols, int(B), float(grad_scale), float(lr),
+            float(beta), int(bool(nesterov)), int(steps), float(update_scale), float(weight_decay), ws, ws_bytes)
+    return theta, m
 
 
 def _flat_f32(name, t, n=None):

@@ -16,6 +16,7 @@ _COMMON = ["pe_host.cuh", "pe_sm100.cuh", "../../include/pestats.h"]
 # each source and the headers it includes
 SOURCES = {
     "pe_api.cu": _COMMON + ["pe_layout.cuh", "pe_optim.cuh", "pe_stage.cuh", "pe_short.cuh", "pe_simt.cuh", "pe_tc.cuh", "pe_tok.cuh"],
+    "pe_muon.cu": _COMMON + ["pe_muon.cuh"],
     "pe_norm.cu": _COMMON + ["pe_norm.cuh"],
 }
 

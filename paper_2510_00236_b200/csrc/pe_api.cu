@@ -2047,7 +2047,7 @@ pe_status_t pe_set_wait_limit_cycles(long long cycles) {
   if (rc != PE_OK) return rc;
   const long long v = cycles > 0 ? cycles : sm100::WAIT_CYCLE_LIMIT_DEFAULT;
   if (cudaMemcpyToSymbol(sm100::g_wait_cycle_limit, &v, sizeof v) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-  return PE_OK;
+  return ns_set_wait_limit(v);
 }
 
 int pe_set_fused_update(int mode) {

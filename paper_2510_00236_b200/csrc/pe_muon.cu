@@ -1,0 +1,175 @@
+// Entry points of the orthogonalised update: argument checks, workspace, and the launches of an iteration.
+#include <algorithm>
+#include <cmath>
+
+#include "pe_host.cuh"
+#include "pe_muon.cuh"
+
+namespace pe {
+
+constexpr int NS_MAX_STEPS = 100;
+constexpr int NS_MAX_PARTIALS = 64;
+
+struct NsLayout {
+  int n, m, ld_m, ld_n, tall;
+  int partials;                    // partial sums of a matrix's norm
+  size_t norms, x[2], a, q, total; // byte offsets into the workspace
+};
+static bool ns_size_ok(int count, int rows, int cols) {
+  return count >= 0 && rows >= 1 && cols >= 1 && rows <= (1 << 30) && cols <= (1 << 30) && (count == 0 || (long long)rows * cols <= ((1ll << 36) - 1) / count) && count <= 65535;
+}
+static NsLayout ns_layout(int count, int rows, int cols) {
+  NsLayout l = {};
+  l.tall = rows > cols;
+  l.n = std::min(rows, cols);
+  l.m = std::max(rows, cols);
+  l.ld_m = (int)align_up(l.m, 8);      // TMA wants row pitches of 16 bytes
+  l.ld_n = (int)align_up(l.n, 8);
+  const long long elems = (long long)rows * cols;
+  l.partials = (int)std::min<long long>(NS_MAX_PARTIALS, (elems + 4095) / 4096);
+  size_t at = 0;
+  auto part = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
+  l.norms = part((size_t)count * l.partials * sizeof(double));
+  for (int k = 0; k < 2; ++k) l.x[k] = part(4ull * count * l.n * l.ld_m);      // two planes of halves
+  l.a = part(4ull * count * l.n * l.ld_n);
+  l.q = part(4ull * count * l.n * l.ld_n);
+  l.total = at;
+  return l;
+}
+
+// Planes [2 * count][rows][ld] of halves, `cols` columns of them data; one box = 64 columns (128 bytes, swizzled) x box_rows rows.
+static pe_status_t ns_map(CUtensorMap* map, const void* base, int planes, int rows, int cols, int ld, int box_rows) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return PE_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
+  cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, estr[3] = {1u, 1u, 1u};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? PE_OK : PE_ERR_CUDA;
+}
+
+template <int NT, bool B_MN, int EPI>
+static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, NsProduct p, cudaStream_t st) {
+  static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];      // devices whose kernel attribute is set
+  auto kernel = ns_product_kernel<NT, B_MN, EPI>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (!(ready[dev >> 6].load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NsTile<NT>::SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    ready[dev >> 6].fetch_or(bit, std::memory_order_release);
+  }
+  const long long tiles_m = (p.rows + 255) / 256;
+  p.tiles_n = (p.cols + NT - 1) / NT;
+  long long units = 0;
+  if (EPI == NS_SYMMETRIC)
+    for (long long i = 0; i < tiles_m; ++i) units += p.tiles_n - i * (256 / NT);
+  else
+    units = tiles_m * p.tiles_n;
+  if (units * p.count >= (1ll << 30)) return PE_ERR_DIM;
+  p.units = (int)units;
+  return launch_dependent(kernel, dim3((unsigned)(2 * units * p.count)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, p);
+}
+
+// The iteration on what `s` describes; `out` holds the last product's output side.
+static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, int rows, int cols, int steps, const NsProduct& out, char* ws, cudaStream_t st) {
+  const NsLayout l = ns_layout(count, rows, cols);
+  double* norms = reinterpret_cast<double*>(ws + l.norms);
+  __half* x[2] = {reinterpret_cast<__half*>(ws + l.x[0]), reinterpret_cast<__half*>(ws + l.x[1])};
+  __half *const a = reinterpret_cast<__half*>(ws + l.a), *const q = reinterpret_cast<__half*>(ws + l.q);
+  pe_status_t rc = launch_dependent(ns_norms_kernel, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms);
+  if (rc != PE_OK) return rc;
+  const int tiles_m = (l.m + NS_INIT_TILE - 1) / NS_INIT_TILE, tiles_n = (l.n + NS_INIT_TILE - 1) / NS_INIT_TILE;
+  rc = launch_dependent(ns_init_kernel, dim3((unsigned)(tiles_m * tiles_n), count), 256, 0, st, s, l.n, l.m, l.ld_m, l.tall, tiles_m, (const double*)norms,
+                        l.partials, x[0], count);
+  if (rc != PE_OK) return rc;
+  constexpr int NT = 128;
+  CUtensorMap xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
+  for (int k = 0; k < 2; ++k)
+    if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, NT / 2) != PE_OK ||
+        ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK) != PE_OK)
+      return PE_ERR_CUDA;
+  if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, NT / 2) != PE_OK ||
+      ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK)
+    return PE_ERR_CUDA;
+  NsProduct p = out;
+  p.count = count;
+  p.dev_status = di->status_ptr;
+  p.chunk = 2;
+  for (int k = 0; k < steps; ++k) {
+    const int from = k & 1;
+    p.rows = p.cols = l.n; p.k = l.m; p.add = nullptr; p.out = a; p.ld = l.ld_n;
+    if ((rc = launch_product<NT, false, NS_SYMMETRIC>(xa[from], xb_rows[from], p, st)) != PE_OK) return rc;
+    p.k = l.n; p.add = a; p.out = q;
+    if ((rc = launch_product<NT, false, NS_SYMMETRIC>(aa, ab, p, st)) != PE_OK) return rc;
+    p.cols = l.m; p.add = nullptr; p.out = x[from ^ 1]; p.ld = l.ld_m;
+    rc = k + 1 < steps ? launch_product<NT, true, NS_PLANES>(qa, xb_cols[from], p, st) : launch_product<NT, true, NS_FINAL>(qa, xb_cols[from], p, st);
+    if (rc != PE_OK) return rc;
+  }
+  return PE_OK;
+}
+
+static pe_status_t ns_check(int count, int rows, int cols, int steps, const void* workspace, size_t workspace_bytes) {
+  if (!ns_size_ok(count, rows, cols) || steps < 1 || steps > NS_MAX_STEPS) return PE_ERR_DIM;
+  if (count == 0) return PE_OK;
+  if (!workspace || workspace_bytes < ns_layout(count, rows, cols).total) return PE_ERR_WORKSPACE;
+  return aligned(workspace, 256) ? PE_OK : PE_ERR_ALIGN;
+}
+
+static pe_status_t orthogonalize_impl(const void* G, int bf16, int count, int rows, int cols, int steps, void* out, void* workspace,
+                                      size_t workspace_bytes, cudaStream_t st) {
+  if ((!G || !out) && count > 0) return PE_ERR_NULL;
+  if (!aligned(G, bf16 ? 16 : 4) || !aligned(out, bf16 ? 16 : 4)) return PE_ERR_ALIGN;
+  pe_status_t rc = ns_check(count, rows, cols, steps, workspace, workspace_bytes);
+  if (rc != PE_OK) return rc;
+  DeviceInfo* di = nullptr;
+  rc = device_info(&di);
+  if (rc != PE_OK || count == 0) return rc;
+  NsSource s = {};
+  s.given = G; s.bf16 = bf16;
+  NsProduct p = {};
+  p.result = out; p.out_bf16 = bf16; p.transposed = rows > cols;
+  return newton_schulz(di, s, count, rows, cols, steps, p, static_cast<char*>(workspace), st);
+}
+
+pe_status_t ns_set_wait_limit(long long cycles) {
+  if (cudaMemcpyToSymbol(sm100::g_wait_cycle_limit, &cycles, sizeof cycles) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  return PE_OK;
+}
+
+}  // namespace pe
+
+using namespace pe;
+
+extern "C" {
+
+size_t pe_orthogonalize_workspace_bytes(int count, int rows, int cols) {
+  return ns_size_ok(count, rows, cols) && count > 0 ? ns_layout(count, rows, cols).total : 0;
+}
+pe_status_t pe_orthogonalize(const void* G, int count, int rows, int cols, int steps, void* out, void* workspace, size_t workspace_bytes,
+                             pe_stream_t stream) {
+  return orthogonalize_impl(G, 1, count, rows, cols, steps, out, workspace, workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+pe_status_t pe_orthogonalize_f32(const float* G, int count, int rows, int cols, int steps, float* out, void* workspace, size_t workspace_bytes,
+                                 pe_stream_t stream) {
+  return orthogonalize_impl(G, 0, count, rows, cols, steps, out, workspace, workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+pe_status_t muon_step(float* theta, void* theta_lp, float* m, const float* sum_g, int count, int rows, int cols, int B, float grad_scale, float lr, float beta,
+                      int nesterov, int steps, float update_scale, float weight_decay, void* workspace, size_t workspace_bytes, pe_stream_t stream) {
+  if ((!theta || !m || !sum_g) && count > 0) return PE_ERR_NULL;
+  if (B < 1) return PE_ERR_DIM;
+  if (!aligned(theta, 16) || !aligned(m, 16) || !aligned(sum_g, 16) || !aligned(theta_lp, 16)) return PE_ERR_ALIGN;
+  pe_status_t rc = ns_check(count, rows, cols, steps, workspace, workspace_bytes);
+  if (rc != PE_OK) return rc;
+  DeviceInfo* di = nullptr;
+  rc = device_info(&di);
+  if (rc != PE_OK || count == 0) return rc;
+  NsSource s = {};
+  s.m = m; s.sum_g = sum_g; s.grad_scale = (float)((double)grad_scale / (double)B); s.beta = beta; s.nesterov = nesterov != 0;
+  NsProduct p = {};
+  p.theta = theta; p.theta_lp = static_cast<__nv_bfloat16*>(theta_lp); p.step = lr * update_scale; p.wd = weight_decay; p.transposed = rows > cols;
+  return newton_schulz(di, s, count, rows, cols, steps, p, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,406 @@
+// Orthogonalised updates: the quintic Newton-Schulz iteration on matrices, and the optimizer step around it.
+//
+//     X = U / ||U||_F  (n x m, n the shorter side: a tall matrix is transposed),   then `steps` times
+//     A = X X^T,   Q = a I + b A + c A A,   X <- Q X          (a, b, c) = (3.4445, -4.7750, 2.0315)
+// which applies a s + b s^3 + c s^5 to the singular values and leaves the singular vectors.  It maps [0, 1.2025] into itself, so every
+// |entry| of X is at most 1.21, of A 1.45, of Q 3.45.
+//
+// The iteration multiplies what is off by its slope, up to 3.4 per step where singular values are small, so operands of 8 or 11 significant
+// bits are off by 1e-2 or 1e-3 afterwards (a fifth or 3e-2 where a few directions dominate).  Operands are therefore kept as two IEEE halves, v = hi + lo
+// (22 bits, scaled by 2^12 so that neither is subnormal where it matters), and a product is hi hi + hi lo + lo hi on the
+// tensor cores: three times the work of one 16-bit product, and errors like those of an fp32 product.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "pe_sm100.cuh"
+
+namespace pe {
+
+constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
+constexpr float NS_SCALE = 4096.f;                     // planes hold 2^12 v
+constexpr float NS_UNSCALE = 1.f / 4096.f;
+
+// hi + lo of an already scaled value
+__device__ __forceinline__ void ns_split(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  lo = __float2half_rn(v - __half2float(hi));
+}
+__device__ __forceinline__ uint32_t ns_pack(__half a, __half b) {
+  const __half2 h = __halves2half2(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---------------------------------------------------------------- momentum, norms, the first operand
+// What the iteration starts from: a matrix as given (bf16 or fp32), or the momentum after this step.
+struct NsSource {
+  const void* given;          // given matrices, or NULL: momentum
+  int bf16;
+  float* m;                   // momentum, updated by ns_norms_kernel
+  const float* sum_g;
+  float grad_scale, beta;     // grad_scale = s / B
+  int nesterov;
+};
+__device__ __forceinline__ float ns_source_value(const NsSource& s, long long i) {      // after ns_norms_kernel
+  if (s.given) return s.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.given)[i]) : static_cast<const float*>(s.given)[i];
+  const float m = s.m[i];
+  return s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * (s.sum_g[i] * s.grad_scale)) : m;
+}
+// Squared Frobenius norms, as gridDim.x partial sums per matrix (gridDim.y matrices), in 64 bits: no scale of the gradients overflows or vanishes.
+// Updates the momentum by the way.
+constexpr int NS_NORM_THREADS = 256;
+__global__ void __launch_bounds__(NS_NORM_THREADS)
+ns_norms_kernel(NsSource s, long long elems, double* __restrict__ partial) {
+  sm100::griddep_launch_dependents();
+  sm100::griddep_wait();
+  __shared__ double warp_sum[NS_NORM_THREADS / 32];
+  const long long base = (long long)blockIdx.y * elems, stride = (long long)gridDim.x * blockDim.x;
+  double sum = 0.0;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < elems; i += stride) {
+    if (!s.given) s.m[base + i] = fmaf(s.beta, s.m[base + i], (1.f - s.beta) * (s.sum_g[base + i] * s.grad_scale));
+    const double v = ns_source_value(s, base + i);
+    sum += v * v;
+  }
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double t = 0.0;
+    for (int w = 0; w < NS_NORM_THREADS / 32; ++w) t += warp_sum[w];
+    partial[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = t;
+  }
+}
+// X = U / ||U||_F as planes [2][count][n][ld]; a block takes 64 x 64 of it.  tall: U is [m, n] and goes through shared memory transposed.
+// ||U|| = 0 gives X = 0.
+constexpr int NS_INIT_TILE = 64;
+__global__ void __launch_bounds__(256)
+ns_init_kernel(NsSource s, int n, int m, int ld, int tall, int tiles_m, const double* __restrict__ partial, int partials, __half* __restrict__ planes,
+               int count) {
+  sm100::griddep_launch_dependents();
+  sm100::griddep_wait();
+  __shared__ float tile[NS_INIT_TILE][NS_INIT_TILE + 1];      // [row of X][column of X]
+  __shared__ double inverse;
+  const int mat = blockIdx.y, r0 = (int)(blockIdx.x / tiles_m) * NS_INIT_TILE, c0 = (int)(blockIdx.x % tiles_m) * NS_INIT_TILE;
+  if (threadIdx.x < 32) {
+    double t = 0.0;
+    for (int k = threadIdx.x; k < partials; k += 32) t += partial[(size_t)mat * partials + k];
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) t += __shfl_xor_sync(0xffffffffu, t, k);
+    if (threadIdx.x == 0) inverse = t == 0.0 ? 0.0 : (double)NS_SCALE / sqrt(t);
+  }
+  __syncthreads();
+  const double inv = inverse;
+  const long long base = (long long)mat * n * m;
+  const int fast = threadIdx.x & 63, slow = threadIdx.x >> 6;
+#pragma unroll 4
+  for (int k = slow; k < NS_INIT_TILE; k += 4) {
+    const int r = tall ? fast : k, c = tall ? k : fast;
+    float v = 0.f;
+    if (r0 + r < n && c0 + c < m)
+      v = (float)(inv * (double)ns_source_value(s, base + (tall ? (long long)(c0 + c) * n + r0 + r : (long long)(r0 + r) * m + c0 + c)));
+    tile[r][c] = v;
+  }
+  __syncthreads();
+  const size_t plane = (size_t)count * n * ld;
+  for (int k = threadIdx.x; k < NS_INIT_TILE * NS_INIT_TILE / 8; k += 256) {
+    const int r = k >> 3, c = (k & 7) * 8;
+    if (r0 + r >= n || c0 + c >= ld) continue;      // (ld is a multiple of 8: columns from m on are written with zeros)
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      __half h0, l0, h1, l1;
+      ns_split(tile[r][c + 2 * e], h0, l0);
+      ns_split(tile[r][c + 2 * e + 1], h1, l1);
+      hi[e] = ns_pack(h0, h1);
+      lo[e] = ns_pack(l0, l1);
+    }
+    __half* at = planes + ((size_t)mat * n + r0 + r) * ld + c0 + c;
+    *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(at + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  }
+}
+
+// ---------------------------------------------------------------- products
+// A pair of thread blocks contracts one 256 x NT tile of one matrix.  Warp 0 of each block feeds its share of the operands by TMA (both
+// planes of 64 values of the contraction index per stage), warp 1 of the leader issues the MMAs, eight warps per block add up what is in
+// tensor memory and write the tile out.
+//
+// The tensor cores add to their fp32 accumulator by truncation, which pulls long sums of one sign (the diagonal of A) towards zero, a
+// little per instruction.  So an accumulator takes `chunk` stages, the small cross terms before hi hi, and the chunks are added
+// up in registers, rounded to nearest: two accumulators in turn, drained while the other one fills.
+enum : int { NS_SYMMETRIC = 0, NS_PLANES = 1, NS_FINAL = 2 };
+struct NsProduct {
+  int rows, cols, k;             // of the product: [rows, cols], contracted over k
+  int tiles_n;                   // column tiles; NS_SYMMETRIC: those that touch the upper triangle are worked on
+  int units;                     // tiles per matrix
+  int count, chunk;
+  const __half* add;             // NS_SYMMETRIC: NULL, or planes [2][count][rows][ld] of A: the result is a I + b A + c (product)
+  __half* out;                   // planes [2][count][rows][ld]
+  int ld;
+  // NS_FINAL: the result itself, [rows, cols] per matrix, or transposed: [cols, rows]
+  int transposed, out_bf16;
+  void* result;                  // as given, or NULL and
+  float* theta;                  // theta <- theta - step X - wd theta
+  __nv_bfloat16* theta_lp;
+  float step, wd;
+  unsigned int* dev_status;
+};
+constexpr int NS_THREADS = 320;
+constexpr int NS_BK = 64;
+constexpr int NS_TMEM_COLS = 512;
+template <int NT>
+struct NsTile {
+  static constexpr int A_PLANE = 128 * 128;                  // 128 rows of 64 halves
+  static constexpr int B_PLANE = (NT / 2) * 128;
+  static constexpr int STAGE_BYTES = 2 * A_PLANE + 2 * B_PLANE;
+  static constexpr int STAGES = NT == 256 ? 3 : 4;
+  static constexpr int BAR_BYTES = 256;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + BAR_BYTES + 1024;
+};
+enum : int { NS_WAIT_EMPTY = 101, NS_WAIT_FULL = 102, NS_WAIT_ACC_EMPTY = 103, NS_WAIT_ACC_FULL = 104 };
+
+// Instruction descriptor: IEEE half operands, A row by row (K-major), B row by row or (b_mn) with the contraction index slow.
+__host__ __device__ constexpr uint32_t ns_idesc(int N, bool b_mn) {
+  return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+}
+
+// One thread's row `r`, columns c .. c + 31 of the tile: scaled values to both planes, and to their mirror image.
+__device__ __forceinline__ void ns_store_planes(const NsProduct& p, size_t mat_row0, int r, int c, const float (&v)[32], bool symmetric) {
+  const size_t plane = (size_t)p.count * p.rows * p.ld;
+#pragma unroll
+  for (int j = 0; j < 32; j += 8) {
+    if (c + j >= p.cols) continue;
+    __half hi[8], lo[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ns_split(v[j + e], hi[e], lo[e]);
+    if (r < p.rows) {
+      __half* at = p.out + (mat_row0 + r) * p.ld + c + j;
+      if (!symmetric || c + j >= r) {
+        *reinterpret_cast<uint4*>(at) = make_uint4(ns_pack(hi[0], hi[1]), ns_pack(hi[2], hi[3]), ns_pack(hi[4], hi[5]), ns_pack(hi[6], hi[7]));
+        *reinterpret_cast<uint4*>(at + plane) = make_uint4(ns_pack(lo[0], lo[1]), ns_pack(lo[2], lo[3]), ns_pack(lo[4], lo[5]), ns_pack(lo[6], lo[7]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + j + e >= r) { at[e] = hi[e]; at[plane + e] = lo[e]; }
+      }
+      if (symmetric) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + j + e > r && c + j + e < p.rows) {
+            __half* mirror = p.out + (mat_row0 + c + j + e) * p.ld + r;
+            mirror[0] = hi[e];
+            mirror[plane] = lo[e];
+          }
+      }
+    }
+  }
+}
+
+template <int NT, bool B_MN, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NS_THREADS, 1)
+ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ NsProduct p) {
+  using namespace sm100;
+  using Tile = NsTile<NT>;
+  constexpr int STAGES = Tile::STAGES, ACC = 2, COLS = NT / 2;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t bar_base = smem_base + STAGES * Tile::STAGE_BYTES;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+  auto acc_full_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + a); };
+  auto acc_empty_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + ACC + a); };
+  uint8_t* tail = smem_gen + STAGES * Tile::STAGE_BYTES + 8 * (2 * STAGES + 2 * ACC);
+  static_assert(8 * (2 * STAGES + 2 * ACC) + 16 <= Tile::BAR_BYTES, "barrier area too small");
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const long long unit = blockIdx.x >> 1;
+  const int mat = (int)(unit / p.units);
+  int tile_m = 0, tile_n = (int)(unit - (long long)mat * p.units);
+  if constexpr (EPI == NS_SYMMETRIC) {      // row by row, the tiles from the diagonal on
+    constexpr int PER = 256 / NT;
+    while (tile_n >= p.tiles_n - tile_m * PER) { tile_n -= p.tiles_n - tile_m * PER; ++tile_m; }
+    tile_n += tile_m * PER;
+  } else {
+    tile_m = tile_n / p.tiles_n;
+    tile_n -= tile_m * p.tiles_n;
+  }
+  const int stages = (p.k + NS_BK - 1) / NS_BK, n_acc = (stages + p.chunk - 1) / p.chunk;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < ACC; ++a) { mbar_init(acc_full_bar(a), 1); mbar_init(acc_empty_bar(a), 16); }
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) { tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), NS_TMEM_COLS); tmem_relinquish_pair(); }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  griddep_launch_dependents();
+  griddep_wait();
+
+  if (warp == 0) {
+    // ---------------------------------------------------------- TMA producer (both blocks)
+    const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
+    int s = 0;
+    uint32_t ph = 1;
+    for (int ks = 0; ks < stages; ++ks) {
+      if (!mbar_wait_warp(empty_bar(s), ph, abort_flag, p.dev_status, NS_WAIT_EMPTY, strict)) break;
+      if (elect_one()) {
+        if (rank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * Tile::STAGE_BYTES);
+        const uint32_t leader_full = map_to_cta(full_bar(s), 0), dst = smem_base + s * Tile::STAGE_BYTES;
+        const int k0 = ks * NS_BK, row = tile_m * 256 + (int)rank * 128, col = tile_n * NT + (int)rank * (NT / 2);
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane) {
+          const int z = plane * p.count + mat;
+          tma_load_3d_pair(dst + plane * Tile::A_PLANE, &map_a, leader_full, k0, row, z);
+          const uint32_t b = dst + 2 * Tile::A_PLANE + plane * Tile::B_PLANE;
+          if constexpr (B_MN) {
+#pragma unroll
+            for (int j = 0; j < NT / 128; ++j) tma_load_3d_pair(b + j * (NS_BK * 128), &map_b, leader_full, col + 64 * j, k0, z);
+          } else {
+            tma_load_3d_pair(b, &map_b, leader_full, k0, col, z);
+          }
+        }
+      }
+      __syncwarp();
+      if (++s == STAGES) { s = 0; ph ^= 1u; }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------- MMA issuer (leader block)
+    if (rank == 0) {
+      const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
+      const uint32_t idesc = ns_idesc(NT, B_MN);
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int ks = 0; ks < stages && ok; ++ks) {
+        const int a = ks / p.chunk, in_chunk = ks - a * p.chunk, buf = a % ACC;
+        if (in_chunk == 0) {
+          if (!mbar_wait_warp(acc_empty_bar(buf), ((uint32_t)(a / ACC) & 1u) ^ 1u, abort_flag, p.dev_status, NS_WAIT_ACC_EMPTY, strict)) { ok = false; break; }
+          tc_fence_after();
+        }
+        if (!mbar_wait_warp(full_bar(s), ph, abort_flag, p.dev_status, NS_WAIT_FULL, strict)) { ok = false; break; }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t d_tmem = tmem_base + (uint32_t)(buf * NT);
+          const uint32_t a_src = smem_base + s * Tile::STAGE_BYTES, b_src = a_src + 2 * Tile::A_PLANE;
+          uint32_t accumulate = in_chunk > 0;
+          const int k_left = p.k - ks * NS_BK;
+#pragma unroll
+          for (int term = 0; term < 3; ++term) {        // hi lo, lo hi, hi hi
+            const uint32_t ap = a_src + (term == 1 ? Tile::A_PLANE : 0), bp = b_src + (term == 0 ? Tile::B_PLANE : 0);
+#pragma unroll
+            for (int k = 0; k < NS_BK / 16; ++k) {
+              if (k * 16 < k_left) {
+                const uint64_t ad = make_smem_desc(ap + k * 32, 16u, 1024u, 2u);
+                const uint64_t bd = B_MN ? make_smem_desc(bp + k * 2048, NS_BK * 128, 1024u, 2u) : make_smem_desc(bp + k * 32, 16u, 1024u, 2u);
+                umma_ss_pair<0>(d_tmem, ad, bd, idesc, accumulate);
+                accumulate = 1;
+              }
+            }
+          }
+          umma_commit_pair(empty_bar(s));
+          if (ks == stages - 1 || in_chunk == p.chunk - 1) umma_commit_pair(acc_full_bar(buf));
+        }
+        __syncwarp();
+        if (++s == STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else {
+    // ---------------------------------------------------------- epilogue (both blocks)
+    const int q = warp & 3, h = (warp - 2) >> 2;      // lanes of tensor memory that this warp may read, half of the columns
+    const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
+    const int r = tile_m * 256 + (int)rank * 128 + q * 32 + lane, c0 = tile_n * NT + h * COLS;
+    float acc[COLS];
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
+    bool ok = true;
+    for (int a = 0; a < n_acc; ++a) {
+      const int buf = a % ACC;
+      if (!mbar_wait_warp(acc_full_bar(buf), (uint32_t)(a / ACC) & 1u, abort_flag, p.dev_status, NS_WAIT_ACC_FULL)) { ok = false; break; }
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < COLS / 32; ++c) {
+        uint32_t v[32];
+        tmem_ld_32x32b_x32_wait(lane_base + (uint32_t)(buf * NT + h * COLS + c * 32), v);
+        if (c == COLS / 32 - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar(buf), 0));
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) acc[c * 32 + j] += __uint_as_float(v[j]);
+      }
+    }
+    if (ok && EPI == NS_FINAL) ok = *reinterpret_cast<volatile unsigned int*>(p.dev_status) == 0u;      // an earlier product may have given up
+    if (ok) {
+#pragma unroll
+      for (int c = 0; c < COLS / 32; ++c) {
+        const int col = c0 + c * 32;
+        if (col < p.cols) {      // (the warp as one)
+          float v[32];
+          if constexpr (EPI == NS_FINAL) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * (NS_UNSCALE * NS_UNSCALE);
+            if (r < p.rows) {
+              const size_t base = (size_t)mat * p.rows * p.cols;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                if (col + j < p.cols) {
+                  const size_t at = base + (p.transposed ? (size_t)(col + j) * p.rows + r : (size_t)r * p.cols + col + j);
+                  if (p.result) {
+                    if (p.out_bf16) static_cast<__nv_bfloat16*>(p.result)[at] = __float2bfloat16_rn(v[j]);
+                    else static_cast<float*>(p.result)[at] = v[j];
+                  } else {
+                    const float th = p.theta[at], next = th - p.step * v[j] - p.wd * th;
+                    p.theta[at] = next;
+                    if (p.theta_lp) p.theta_lp[at] = __float2bfloat16_rn(next);
+                  }
+                }
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * NS_UNSCALE;      // 2^12 of the value
+            const size_t row0 = (size_t)mat * p.rows;
+            if constexpr (EPI == NS_SYMMETRIC) {
+              if (p.add && r < p.rows) {
+                const size_t plane = (size_t)p.count * p.rows * p.ld;
+                const __half* at = p.add + (row0 + r) * p.ld + col;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                  const bool in = col + j < p.cols;
+                  const float A = in ? __half2float(at[j]) + __half2float(at[plane + j]) : 0.f;
+                  v[j] = fmaf(NS_C, v[j], fmaf(NS_B, A, r == col + j ? NS_A * NS_SCALE : 0.f));
+                }
+              }
+            }
+            ns_store_planes(p, row0, r, col, v, EPI == NS_SYMMETRIC);
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {      // a wait gave up: loads in flight may still land here, so the block stays a while
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
+  }
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, NS_TMEM_COLS); }
+}
+
+}  // namespace pe
