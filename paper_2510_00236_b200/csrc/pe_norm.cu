@@ -1,5 +1,6 @@
 // Entry points of the normalisation layers: argument checks, the choice of the launch, and the launches.
 #include <algorithm>
+#include <type_traits>
 
 #include "pe_host.cuh"
 #include "pe_norm.cuh"
@@ -19,7 +20,7 @@ static ForwardPlan plan_forward(int d, int E) {
     while (p.G < vectors) p.G *= 2;
   } else if (vectors <= 256) {
     while (p.nv * 32 < vectors) p.nv *= 2;
-  } else if (vectors <= 8192) {
+  } else if (vectors <= 4096) {
     p.nv = 8;
     p.G = (vectors + 255) / 256 * 32;
   } else {
@@ -38,14 +39,22 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
   if (p.G == 0)
     return launch_dependent(norm_forward_wide_kernel<T, RMS>, dim3((unsigned)std::min<long long>(rows, 2ll * di->sm_count)), p.threads, 0, st, x, gain,
                             bias, rows, d, eps, y, mean, rstd);
-  const int groups = p.threads / p.G;
-  const long long blocks = (rows + groups - 1) / groups;
-  const dim3 grid((unsigned)std::min<long long>(blocks, 1 << 30));
+  const int wide = aligned(gain, 16) && aligned(bias, 16);
+  // two rows at a time where enough of them remain to fill the device
+  const int groups = p.threads / p.G, r = p.G <= 32 && rows >= 64ll * di->sm_count ? 2 : 1;
+  const long long blocks = (rows + (long long)groups * r - 1) / ((long long)groups * r);
+  if (blocks >= (1ll << 31)) return PE_ERR_DIM;
+  const dim3 grid((unsigned)blocks);
+  auto run = [&](auto nv) {
+    constexpr int NV = decltype(nv)::value;
+    if (r == 2) return launch_dependent(norm_forward_kernel<T, E, NV, 2, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
+    return launch_dependent(norm_forward_kernel<T, E, NV, 1, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
+  };
   switch (p.nv) {
-    case 1: return launch_dependent(norm_forward_kernel<T, E, 1, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
-    case 2: return launch_dependent(norm_forward_kernel<T, E, 2, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
-    case 4: return launch_dependent(norm_forward_kernel<T, E, 4, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
-    default: return launch_dependent(norm_forward_kernel<T, E, 8, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G);
+    case 1: return run(std::integral_constant<int, 1>{});
+    case 2: return run(std::integral_constant<int, 2>{});
+    case 4: return run(std::integral_constant<int, 4>{});
+    default: return run(std::integral_constant<int, 8>{});
   }
 }
 
@@ -74,13 +83,13 @@ static pe_status_t forward_impl(const T* x, const float* gain, const float* bias
 }
 
 // ---------------------------------------------------------------- backward
-constexpr int NORM_WHOLE_THREADS = 512;      // a block of the one-pass kernel: rows of up to 4096 features
+constexpr int NORM_WHOLE_THREADS = NORM_MAX_THREADS;      // a block of the one-pass kernel: rows of up to 4096 features
 constexpr int NORM_SLAB_THREADS = 256;       // a block of the two-pass kernel: 2048 features
 constexpr int NORM_SM_COUNT = 148;           // the workspace is sized for launches of at most this many SMs
 struct BackwardPlan {
   bool whole;
   int G, groups, blocks, slabs;              // blocks along the rows; slabs of features (two-pass)
-  size_t ends_at, means_at, bytes;           // workspace: elements, their flags, the rows' means
+  size_t ends_at, heads_at, means_at, bytes; // workspace: elements, their flags, heads, the rows' means
 };
 static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count) {
   BackwardPlan p = {};
@@ -102,7 +111,8 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
   const long long most = p.whole ? sm_count * std::max(1, 512 / (p.G * p.groups)) : std::max(1, 2 * sm_count / p.slabs);
   p.blocks = (int)std::min(want, most);
   p.ends_at = align_up((size_t)p.blocks * NORM_PARTS * kinds * d * sizeof(float), 256);
-  p.means_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
+  p.heads_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
+  p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
   p.bytes = p.means_at + (p.whole ? 0 : align_up((size_t)rows * sizeof(float2), 256));
   return p;
 }
@@ -110,26 +120,31 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
 template <typename T, int E, bool RMS, int KINDS>
 static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, const BackwardPlan& p, char* ws, cudaStream_t st) {
   const int threads = p.G * p.groups;
-  const int smem = (int)(((size_t)threads * NORM_PARTS * NORM_COLS) * sizeof(float) + p.groups * sizeof(int));
+  // the ring and its barriers, and in the same place later the workers' elements
+  const size_t slot = norm_slot_bytes(norm_rows<T>(), p.whole ? a.d : p.G * NORM_COLS, sizeof(T), p.whole);
+  const int smem = (int)std::max((size_t)p.groups * NORM_STAGES * (2 * slot + 8), (size_t)threads * NORM_PARTS * KINDS * NORM_COLS * sizeof(float));
   a.G = p.G;
   a.parts = reinterpret_cast<float*>(ws);
   a.ends = reinterpret_cast<int*>(ws + p.ends_at);
+  a.heads = reinterpret_cast<float*>(ws + p.heads_at);
+  a.dev_status = di->status_ptr;
   a.row_means = reinterpret_cast<const float2*>(ws + p.means_at);
   auto large_smem = [&](auto kernel) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess ? PE_OK : (cudaGetLastError(), PE_ERR_CUDA);
   };
-  if (p.whole) {
-    auto kernel = norm_backward_kernel<T, E, RMS, KINDS, true, NORM_WHOLE_THREADS>;
+  auto launch = [&](auto kernel) {
     if (smem > 48 * 1024) {
       const pe_status_t rc = large_smem(kernel);
       if (rc != PE_OK) return rc;
     }
-    return launch_dependent(kernel, dim3(p.blocks), threads, smem, st, x, dy, dx, a);
-  }
+    return launch_dependent(kernel, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
+  };
+  if (p.whole)
+    return launch(norm_backward_kernel<T, E, RMS, KINDS, true>);
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
                                           a, reinterpret_cast<float2*>(ws + p.means_at));
   if (rc != PE_OK) return rc;
-  return launch_dependent(norm_backward_kernel<T, E, RMS, KINDS, false, NORM_SLAB_THREADS>, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
+  return launch(norm_backward_kernel<T, E, RMS, KINDS, false>);
 }
 
 template <typename T>
@@ -162,7 +177,7 @@ static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, con
   if (!aligned(workspace, 256)) return PE_ERR_ALIGN;
   NormBackward a = {};
   a.gain = gain; a.mean = mean; a.rstd = rstd; a.offsets = packed ? offsets : nullptr;
-  a.rows = rows; a.B = B; a.T = T_; a.d = d; a.phi = (int)phi;
+  a.wide = aligned(gain, 16); a.rows = rows; a.B = B; a.T = T_; a.d = d; a.phi = (int)phi;
   constexpr int E = 16 / (int)sizeof(T);
   char* ws = static_cast<char*>(workspace);
   const bool vec = d % E == 0 && aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16);

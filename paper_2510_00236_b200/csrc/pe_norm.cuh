@@ -82,9 +82,20 @@ struct NormVec<__nv_bfloat16, E> {      // E = 8: one 16-byte access; E = 1
     }
   }
 };
+// E elements of a gain or bias, which every row's group reads, from L1.  wide: 16-byte aligned (4 bytes suffice for the caller); one float at a time
+// costs as many sectors per load as the whole vector.
 template <int E>
-__device__ __forceinline__ void norm_load_param(const float* p, int col, float (&f)[E]) {
-  // parameters: 4-byte aligned only (E elements of a gain or bias are read by every row's group, from L1)
+__device__ __forceinline__ void norm_load_param(const float* p, int col, bool wide, float (&f)[E]) {
+  if constexpr (E % 4 == 0) {
+    if (wide) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(p + col + e));
+        f[e] = q.x; f[e + 1] = q.y; f[e + 2] = q.z; f[e + 3] = q.w;
+      }
+      return;
+    }
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e) f[e] = __ldg(p + col + e);
 }
@@ -121,75 +132,81 @@ __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, 
 }
 
 // ---------------------------------------------------------------- forward
-// NV vectors of E features per thread: vector i of a thread is features (i G + thread) E ..
-// The row stays in registers between its sums (mean first, then the squared deviations: no cancellation) and the output.
-template <typename T, int E, int NV, bool RMS>
-__global__ void __launch_bounds__(1024)
+// NV vectors of E features per thread: vector i of a thread is features (i G + thread) E ..; R rows at a time share what is loaded of gain and bias.
+// The rows stay in registers between their sums (mean first, then the squared deviations: no cancellation) and the output.
+template <typename T, int E, int NV, int R, bool RMS>
+__global__ void __launch_bounds__(R > 1 ? 256 : 512)
 norm_forward_kernel(const T* __restrict__ x, const float* __restrict__ gain, const float* __restrict__ bias, long long rows, int d, float eps,
-                    T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, int G) {
-  __shared__ float slots[2 * NORM_MAX_WARPS];
+                    T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, int G, int wide) {
+  __shared__ float slots[2 * NORM_MAX_WARPS * R];
   sm100::griddep_launch_dependents();
   sm100::griddep_wait();
   const int group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G;
   const float inv_d = 1.f / (float)d;
   int turn = 0;
-  for (long long base = (long long)blockIdx.x * groups; base < rows; base += (long long)gridDim.x * groups) {
-    const long long row = base + group;
-    const bool live = row < rows;
-    const T* xr = x + row * d;
-    NormVec<T, E> in[NV];
+  const long long row0 = ((long long)blockIdx.x * groups + group) * R;
+  NormVec<T, E> in[R][NV];
+#pragma unroll
+  for (int k = 0; k < R; ++k)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + t) * E;
-      if (live && col < d) in[i].load(xr + col);
-      else in[i].zero();
+      if (row0 + k < rows && col < d) in[k][i].load(x + (row0 + k) * d + col);
+      else in[k][i].zero();
     }
-    float mu = 0.f;
-    if constexpr (!RMS) {
-      float s[1] = {0.f};
+  float mu[R], q[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) mu[k] = q[k] = 0.f;
+  if constexpr (!RMS) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         float f[E];
-        in[i].get(f);
+        in[k][i].get(f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[0] += f[e];
+        for (int e = 0; e < E; ++e) mu[k] += f[e];
       }
-      norm_group_sum<1>(s, G, group, t, slots, turn);
-      mu = s[0] / (float)d;      // rounded once: a row of one value keeps it
-    }
-    float q[1] = {0.f};
+    norm_group_sum<R>(mu, G, group, t, slots, turn);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    for (int k = 0; k < R; ++k) mu[k] = mu[k] / (float)d;      // rounded once: a row of one value keeps it
+  }
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
       if ((i * G + t) * E < d) {
         float f[E];
-        in[i].get(f);
+        in[k][i].get(f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) q[0] = fmaf(f[e] - mu, f[e] - mu, q[0]);
+        for (int e = 0; e < E; ++e) q[k] = fmaf(f[e] - mu[k], f[e] - mu[k], q[k]);
       }
+  norm_group_sum<R>(q, G, group, t, slots, turn);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    q[k] = 1.f / sqrtf(q[k] * inv_d + eps);
+    if (t == 0 && row0 + k < rows) {
+      if (!RMS && mean) mean[row0 + k] = mu[k];
+      if (rstd) rstd[row0 + k] = q[k];
     }
-    norm_group_sum<1>(q, G, group, t, slots, turn);
-    const float r = 1.f / sqrtf(q[0] * inv_d + eps);
-    if (live) {
-      if (t == 0) {
-        if (!RMS && mean) mean[row] = mu;
-        if (rstd) rstd[row] = r;
-      }
-      T* yr = y + row * d;
+  }
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int col = (i * G + t) * E;
-        if (col < d) {
-          float f[E], g[E], b[E], o[E];
-          in[i].get(f);
-          if (gain) norm_load_param<E>(gain, col, g);
-          if (bias) norm_load_param<E>(bias, col, b);
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * G + t) * E;
+    if (col < d) {
+      float g[E], b[E];
+      if (gain) norm_load_param<E>(gain, col, wide, g);
+      if (bias) norm_load_param<E>(bias, col, wide, b);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float h = (f[e] - mu) * r;
-            o[e] = gain ? (bias ? fmaf(h, g[e], b[e]) : h * g[e]) : (bias ? h + b[e] : h);
-          }
-          NormVec<T, E>::store(yr + col, o);
+      for (int k = 0; k < R; ++k) {
+        float f[E], o[E];
+        in[k][i].get(f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float h = (f[e] - mu[k]) * q[k];
+          o[e] = gain ? (bias ? fmaf(h, g[e], b[e]) : h * g[e]) : (bias ? h + b[e] : h);
         }
+        if (row0 + k < rows) NormVec<T, E>::store(y + (row0 + k) * d + col, o);
       }
     }
   }
@@ -269,8 +286,11 @@ struct NormBackward {
   const int* offsets;                   // packed batch: B + 1 row offsets; NULL: examples of T rows
   long long rows;                       // rows of the tensors
   int B, T, d, phi, G;                  // G threads per row
+  int wide;                             // gain is 16-byte aligned
   float* parts;                         // [blocks][NORM_PARTS][kinds][d]; a block's element
   int* ends;                            // [blocks]: whether an example ends in the block's rows
+  float* heads;                         // [blocks x slabs][kinds][features of a thread][threads]: workers' heads, kept here until the rows are done
+  unsigned int* dev_status;
   const float2* row_means;              // of each row: (mean(w xh), mean(w)), where a kernel before this one found them
 };
 
@@ -314,165 +334,370 @@ struct NormEnds {
   }
 };
 
-// KINDS: 1 for the gain alone, 2 with the bias.  WHOLE: a group has the whole row and finds the row's two means itself.  Otherwise blockIdx.y picks the features and row_means has them.
-template <typename T, int E, bool RMS, int KINDS, bool WHOLE, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS)
+// The group sum of norm_group_sum for N = 8, 4 or 2 values, by halving exchanges: 9 instead of 40 exchanges for 8 values.  Needs G >= 32.
+template <int N>
+__device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, int thread_in_group, float* slots, int& turn) {
+  const int lane = threadIdx.x & 31;
+  float a[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) a[k] = v[k];
+  int held = N, s = 16;
+#pragma unroll
+  for (int step = 0; step < 5; ++step) {
+    if (held > 1) {      // (compile-time after unrolling) the lane keeps the half of its values that its bit picks
+      const int half = held / 2;
+      const bool high = lane & s;
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k)
+        if (k < half) {
+          const float give = high ? a[k] : a[k + half], keep = high ? a[k + half] : a[k];
+          a[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
+        }
+      held = half;
+    } else {
+      a[0] += __shfl_xor_sync(0xffffffffu, a[0], s);
+    }
+    s >>= 1;
+  }
+  // lane bits 4, 3, .. pick value bits log2(N) - 1, ..
+  constexpr int SHIFT = N == 8 ? 2 : N == 4 ? 3 : 4;
+  if (G > 32) {
+    const int warps = G >> 5, first = group * warps;
+    float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
+    if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = 0.f;
+    for (int w = 0; w < warps; ++w) {
+#pragma unroll
+      for (int k = 0; k < N; k += 2) {
+        const float2 q = *reinterpret_cast<const float2*>(slot + (first + w) * N + k);
+        v[k] += q.x; v[k + 1] += q.y;
+      }
+    }
+    turn ^= 1;
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, a[0], k << SHIFT);
+  }
+}
+
+// KINDS: 1 for the gain alone, 2 with the bias.  WHOLE: a group has the whole row and finds the row's two means itself.  Otherwise
+// blockIdx.y picks the features and row_means has them.
+//
+// A worker's rows come through a ring in shared memory, NORM_STAGES slots of R rows, filled by bulk copies that the group's first thread issues two slots
+// ahead: 128 KB in flight on an SM without a register spent on them, whatever the rows' alignment.  (With the next row's loads in registers,
+// 264 MB of bf16 rows of 2048 features took 1467 us, a third of the copy rate: too little in flight.)  One barrier serves the sums of R rows, and tells that the slot
+// before has been read.  Arithmetic is on pairs of features, one instruction for both; with c = x - mu,
+//     mean(w xh) = r mean(w c),   dx = w r + c (-r^3 mean(w c)) - r mean(w),   G += (dy r) c.
+constexpr int NORM_STAGES = 3;
+template <typename T> __host__ __device__ constexpr int norm_rows() { return sizeof(T) == 2 ? 4 : 2; }      // R: a slot of 256 threads is 32 KB
+enum : int { NORM_WAIT_ROWS = 201 };
+
+// Bytes of a slot: R rows of one tensor and what alignment to 16 bytes adds at both ends (slab: of every row).
+__host__ __device__ constexpr size_t norm_slot_bytes(int R, int cols, int elem, bool whole) {
+  return whole ? (((size_t)R * cols * elem + 15) / 16 * 16 + 32) : (size_t)R * (((size_t)cols * elem + 15) / 16 * 16 + 32);
+}
+
+// Copies n bytes from global memory at `src` to shared memory at dst + (src & 15), dst 16-byte aligned: the 16-byte aligned part by a bulk copy
+// counted on `bar`, whose bytes are returned; begin, end: the tensor.  Only where an aligned word reaches out of the tensor its bytes are copied one element at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, const T* src, size_t n, const T* begin, const T* end, uint32_t bar, bool issue) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(src), lo0 = a & ~(uintptr_t)15, hi0 = (a + n + 15) & ~(uintptr_t)15;
+  uintptr_t lo = lo0, hi = hi0;
+  if (lo < reinterpret_cast<uintptr_t>(begin)) lo += 16;
+  if (hi > reinterpret_cast<uintptr_t>(end)) hi -= 16;
+  if (hi < lo) hi = lo;
+  if (!issue) {      // first call: the odd ends, and the number of bytes to expect
+    for (uintptr_t q = a; q < a + n && q < lo; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
+    for (uintptr_t q = hi > a ? hi : a; q < a + n; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
+    return (uint32_t)(hi - lo);
+  }
+  if (hi > lo)
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + (uint32_t)(lo - lo0)), "l"(lo),
+                 "r"((uint32_t)(hi - lo)), "r"(bar) : "memory");
+  return 0;
+}
+
+constexpr int NORM_MAX_THREADS = 512;      // 128 registers a thread: two blocks of 256 threads or one of 512 to an SM
+template <typename T, int E, bool RMS, int KINDS, bool WHOLE>
+__global__ void __launch_bounds__(NORM_MAX_THREADS, 1)
 norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dx, const NormBackward p) {
-  constexpr int NV = NORM_COLS / E;
-  extern __shared__ float smem[];
-  __shared__ float slots[2 * NORM_MAX_WARPS * 2];
-  sm100::griddep_launch_dependents();
-  sm100::griddep_wait();
-  const int G = p.G, d = p.d, group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G;
-  const int col0 = WHOLE ? 0 : blockIdx.y * G * NORM_COLS;
+  using namespace sm100;
+  constexpr int NV = NORM_COLS / E, R = norm_rows<T>(), P = NORM_COLS / 2, SUMS = RMS ? R : 2 * R, S = NORM_STAGES;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ __align__(16) float slots[2 * (NORM_MAX_THREADS / 32) * SUMS];
+  __shared__ int group_end[256];
+  __shared__ int abort_flag;
+  const int G = p.G, d = p.d, group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G, threads = blockDim.x;
+  const int col0 = WHOLE ? 0 : blockIdx.y * G * NORM_COLS, cols = WHOLE ? d : min(d - col0, G * NORM_COLS);
+  const size_t slot = norm_slot_bytes(R, WHOLE ? d : G * NORM_COLS, sizeof(T), WHOLE);
+  // [group][stage][x, dy], then a barrier per group and stage
+  uint8_t* ring = smem + (size_t)group * S * 2 * slot;
+  const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + (uint32_t)((size_t)groups * S * 2 * slot) + group * S * 8;
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (t == 0) {
+    for (int s = 0; s < S; ++s) mbar_init(bars + 8 * s, 1);
+    fence_barrier_init();
+  }
+  griddep_launch_dependents();
+  griddep_wait();
   long long first, last;
   norm_span(p, first, last);
   const long long workers = (long long)gridDim.x * groups, me = (long long)blockIdx.x * groups + group, span = last - first;
   // (span < 2^40 and workers < 2^20: the products fit)
   const long long r0 = first + span * me / workers, r1 = first + span * (me + 1) / workers;
-  const long long longest = (span + workers - 1) / workers;      // every group of the block takes as many turns
-  float gain[NV][E];
+  const int turns = (int)((span + workers * R - 1) / (workers * R)) ;      // every group of the block takes as many
+  __syncthreads();
+  // the group's first thread: rows r0 + b R .. into slot b % S
+  auto issue = [&](int b) {
+    const long long row = r0 + (long long)b * R;
+    if (row >= r1) return;
+    const int n = (int)min((long long)R, r1 - row), s = b % S;
+    const uint32_t bar = bars + 8 * s;
+    const T *const x_end = x + p.rows * d, *const y_end = dy + p.rows * d;
+    const size_t at = (size_t)s * 2 * slot, row_slot = slot / R;
+    uint32_t bytes = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = col0 + (i * G + t) * E;
+    for (int pass = 0; pass < 2; ++pass) {
+      if constexpr (WHOLE) {
+        bytes += norm_fetch(ring_s + (uint32_t)at, ring + at, x + row * d, (size_t)n * d * sizeof(T), x, x_end, bar, pass == 1);
+        bytes += norm_fetch(ring_s + (uint32_t)(at + slot), ring + at + slot, dy + row * d, (size_t)n * d * sizeof(T), dy, y_end, bar, pass == 1);
+      } else {
+        for (int k = 0; k < n; ++k) {
+          const size_t ak = at + k * row_slot;
+          bytes += norm_fetch(ring_s + (uint32_t)ak, ring + ak, x + (row + k) * d + col0, (size_t)cols * sizeof(T), x, x_end, bar, pass == 1);
+          bytes += norm_fetch(ring_s + (uint32_t)(ak + slot), ring + ak + slot, dy + (row + k) * d + col0, (size_t)cols * sizeof(T), dy, y_end, bar, pass == 1);
+        }
+      }
+      if (pass == 0) mbar_arrive_expect_tx(bar, bytes);
+    }
+  };
+  if (t == 0)
+    for (int b = 0; b < S - 1; ++b) issue(b);
+  uint64_t gain[P], run[KINDS][P], tot[KINDS][P], stat[KINDS][P];
+  {
+    float f[NV][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) gain[i][e] = 1.f;
-    if (p.gain && col < d) norm_load_param<E>(p.gain, col, gain[i]);
+    for (int i = 0; i < NV; ++i) {
+      const int col = col0 + (i * G + t) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[i][e] = 1.f;
+      if (p.gain && col < d) norm_load_param<E>(p.gain, col, p.wide, f[i]);
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) gain[j] = f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
   }
-  float run[KINDS][NV][E], head[KINDS][NV][E], tot[KINDS][NV][E], stat[KINDS][NV][E];
 #pragma unroll
   for (int k = 0; k < KINDS; ++k)
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) run[k][i][e] = head[k][i][e] = tot[k][i][e] = stat[k][i][e] = 0.f;
+    for (int j = 0; j < P; ++j) run[k][j] = tot[k][j] = stat[k][j] = 0ull;
+  float* heads = p.heads + ((size_t)(blockIdx.y * gridDim.x + blockIdx.x) * KINDS * NORM_COLS) * threads;      // [kind][feature of a thread][thread]
   bool any_end = false;
   NormEnds ends(p, last);
   long long end = r0 < r1 ? ends.find(r0) : last;
   const float inv_d = 1.f / (float)d;
   int turn = 0;
-  for (long long k = 0; k < longest; ++k) {
-    const long long row = r0 + k;
-    const bool live = row < r1;
-    NormVec<T, E> vx[NV], vy[NV];
+  bool waits = true;
+  const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
+  float mu[R], rs[R];
+  float2 means[WHOLE ? 1 : R];
+  auto row_values = [&](int b, float (&m)[R], float (&r)[R], float2 (&w)[WHOLE ? 1 : R]) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const long long row = r0 + (long long)b * R + k;
+      const bool live = row < r1;
+      m[k] = (!RMS && live) ? __ldg(p.mean + row) : 0.f;
+      r[k] = live ? __ldg(p.rstd + row) : 0.f;
+      if constexpr (!WHOLE) w[k] = live ? p.row_means[row] : make_float2(0.f, 0.f);
+    }
+  };
+  row_values(0, mu, rs, means);
+  // a thread's features of row k of the slot, as pairs
+  auto pairs = [&](const uint8_t* tensor_slot, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
+    const uint8_t* base;
+    if constexpr (E > 1) base = tensor_slot + (WHOLE ? (size_t)k * d * sizeof(T) : (size_t)k * (slot / R));
+    else if constexpr (WHOLE) base = tensor_slot + (reinterpret_cast<uintptr_t>(tensor + row * d) & 15) + (size_t)k * d * sizeof(T);
+    else base = tensor_slot + (size_t)k * (slot / R) + (reinterpret_cast<uintptr_t>(tensor + (row + k) * d + col0) & 15);
+    float f[NV][E];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int col = col0 + (i * G + t) * E;
-      if (live && col < d) {
-        vx[i].load(x + row * d + col);
-        vy[i].load(dy + row * d + col);
-      } else {
-        vx[i].zero();
-        vy[i].zero();
-      }
-    }
-    const float mu = (!RMS && live) ? __ldg(p.mean + row) : 0.f;
-    const float r = live ? __ldg(p.rstd + row) : 0.f;
-    float s[2] = {0.f, 0.f};
+      const int c = (i * G + t) * E;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float fx[E], fy[E];
-      vx[i].get(fx);
-      vy[i].get(fy);
+      for (int e = 0; e < E; ++e) f[i][e] = 0.f;
+      if (c < cols) {
+        const T* q = reinterpret_cast<const T*>(base) + c;
+        if constexpr (E == 8) {
+          const uint4 v = *reinterpret_cast<const uint4*>(q);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float h = (fx[e] - mu) * r, w = fy[e] * gain[i][e];
-        s[0] = fmaf(w, h, s[0]);
-        s[1] += w;
-        run[0][i][e] = fmaf(fy[e], h, run[0][i][e]);
-        if constexpr (KINDS > 1) run[1][i][e] += fy[e];
-      }
-    }
-    if constexpr (WHOLE) {
-      norm_group_sum<2>(s, G, group, t, slots, turn);
-      s[0] *= inv_d;
-      s[1] *= inv_d;
-    } else if (live) {
-      const float2 m = p.row_means[row];
-      s[0] = m.x;
-      s[1] = m.y;
-    }
-    if (live) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int col = col0 + (i * G + t) * E;
-        if (col < d) {
-          float fx[E], fy[E], o[E];
-          vx[i].get(fx);
-          vy[i].get(fy);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float h = (fx[e] - mu) * r, w = fy[e] * gain[i][e];
-            const float a = fmaf(-h, s[0], w);
-            o[e] = r * (RMS ? a : a - s[1]);
-          }
-          if (dx) NormVec<T, E>::store(dx + row * d + col, o);
+          for (int h = 0; h < 4; ++h) { f[i][2 * h] = __uint_as_float(w[h] << 16); f[i][2 * h + 1] = __uint_as_float(w[h] & 0xffff0000u); }
+        } else if constexpr (E == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(q);
+          f[i][0] = v.x; f[i][1] = v.y; f[i][2] = v.z; f[i][3] = v.w;
+        } else {
+          f[i][0] = (float)*q;
         }
       }
-      if (row + 1 == end) {      // the example ends with this row
+    }
 #pragma unroll
-        for (int k2 = 0; k2 < KINDS; ++k2)
+    for (int j = 0; j < P; ++j) o[j] = f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
+  };
+  for (int b = 0; b < turns; ++b) {
+    const long long row0 = r0 + (long long)b * R;
+    const int sl = b % S;
+    const uint8_t *const sx = ring + (size_t)sl * 2 * slot, *const sy = sx + slot;
+    if (waits && row0 < r1) waits = mbar_wait_bounded(bars + 8 * sl, (uint32_t)(b / S) & 1u, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
+    __syncwarp();
+    float s[SUMS];
 #pragma unroll
-          for (int i = 0; i < NV; ++i)
+    for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float g = run[k2][i][e];
+    for (int k = 0; k < R; ++k) {
+      if (row0 + k < r1) {
+        uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
+        pairs(sx, x, row0, k, fx);
+        pairs(sy, dy, row0, k, fy);
+        const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          const uint64_t c = RMS ? fx[j] : f32x2_sub(fx[j], m2);
+          if constexpr (WHOLE) {
+            const uint64_t w = f32x2_mul(fy[j], gain[j]);
+            s0 = f32x2_fma(w, c, s0);
+            if constexpr (!RMS) s1 = f32x2_add(s1, w);
+          }
+          run[0][j] = f32x2_fma(f32x2_mul(fy[j], r2), c, run[0][j]);
+          if constexpr (KINDS > 1) run[1][j] = f32x2_add(run[1][j], fy[j]);
+        }
+        float lo, hi;
+        f32x2_unpack(s0, lo, hi);
+        s[k] = lo + hi;
+        if constexpr (!RMS) {
+          f32x2_unpack(s1, lo, hi);
+          s[R + k] = lo + hi;
+        }
+        if (row0 + k + 1 == end) {      // the example ends with this row
+#pragma unroll
+          for (int q = 0; q < KINDS; ++q)
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+              float g0, g1;
+              f32x2_unpack(run[q][j], g0, g1);
               if (!any_end) {
-                head[k2][i][e] = g;
+                heads[(q * NORM_COLS + 2 * j) * threads + threadIdx.x] = g0;
+                heads[(q * NORM_COLS + 2 * j + 1) * threads + threadIdx.x] = g1;
               } else {
-                tot[k2][i][e] += g;
-                stat[k2][i][e] += norm_phi(p.phi, g);
+                tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
+                stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g0), norm_phi(p.phi, g1)));
               }
-              run[k2][i][e] = 0.f;
+              run[q][j] = 0ull;
             }
-        any_end = true;
-        end = ends.after(end);
+          any_end = true;
+          end = ends.after(end);
+        }
       }
     }
+    float nm[R], nr[R];
+    float2 nw[WHOLE ? 1 : R];
+    row_values(b + 1, nm, nr, nw);
+    if constexpr (WHOLE) {
+      if (G > 32) norm_rows_sum<SUMS>(s, G, group, t, slots, turn);
+      else norm_group_sum<SUMS>(s, G, group, t, slots, turn);
+    } else {
+      __syncthreads();
+    }
+    __syncwarp();
+    // every thread of the group has left the slot before this one
+    if (t == 0) issue(b + S - 1);
+    if (dx) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const long long row = row0 + k;
+        if (row < r1) {
+          float k0 = 0.f, k1;
+          if constexpr (WHOLE) {
+            k1 = -rs[k] * (rs[k] * (rs[k] * (s[k] * inv_d)));      // (s: sums of w c)
+            if constexpr (!RMS) k0 = -rs[k] * (s[R + k] * inv_d);
+          } else {
+            k1 = -rs[k] * (rs[k] * means[k].x);
+            if constexpr (!RMS) k0 = -rs[k] * means[k].y;
+          }
+          uint64_t fx[P], fy[P];
+          pairs(sx, x, row0, k, fx);
+          pairs(sy, dy, row0, k, fy);
+          const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
+          float o[NV][E];
+#pragma unroll
+          for (int j = 0; j < P; ++j) {
+            const uint64_t c = RMS ? fx[j] : f32x2_sub(fx[j], m2), w = f32x2_mul(fy[j], gain[j]);
+            const uint64_t v = f32x2_fma(c, k12, RMS ? f32x2_mul(w, r2) : f32x2_fma(w, r2, k02));
+            f32x2_unpack(v, o[2 * j / E][2 * j % E], o[(2 * j + 1) / E][(2 * j + 1) % E]);
+          }
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const int col = (i * G + t) * E;
+            if (col < cols) NormVec<T, E>::store(dx + row * d + col0 + col, o[i]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      mu[k] = nm[k];
+      rs[k] = nr[k];
+      if constexpr (!WHOLE) means[k] = nw[k];
+    }
   }
-  // this worker's element: without an end all of its sum is `head`
+  // The ring has been read for the last time: it holds the workers' elements now, part q, kind k, feature c of every thread.
+  __syncthreads();
+  if (abort_flag) {      // a wait gave up: copies in flight may still land here
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
+  }
+  float* words = reinterpret_cast<float*>(smem);
+  auto word = [&](int q, int k, int c, int thread) -> float& { return words[((q * KINDS + k) * NORM_COLS + c) * threads + thread]; };
 #pragma unroll
   for (int k = 0; k < KINDS; ++k)
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int j = 0; j < P; ++j) {
+      float g[2], a[2], v[2];
+      f32x2_unpack(run[k][j], g[0], g[1]);
+      f32x2_unpack(tot[k][j], a[0], a[1]);
+      f32x2_unpack(stat[k][j], v[0], v[1]);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (!any_end) { head[k][i][e] = run[k][i][e]; run[k][i][e] = 0.f; }
-  // The block's groups are joined by way of shared memory, one (kind) at a time: [groups][NORM_PARTS][G * 8].
-  int* group_end = reinterpret_cast<int*>(smem + (size_t)groups * NORM_PARTS * G * NORM_COLS);
-  if (t == 0) group_end[group] = any_end;
-  const int width = G * NORM_COLS;
-#pragma unroll
-  for (int k = 0; k < KINDS; ++k) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float* at = smem + (size_t)group * NORM_PARTS * width + (i * G + t) * E + e;
-        at[NORM_HEAD * width] = head[k][i][e];
-        at[NORM_TOT * width] = tot[k][i][e];
-        at[NORM_STAT * width] = stat[k][i][e];
-        at[NORM_TAIL * width] = run[k][i][e];
+      for (int e = 0; e < 2; ++e) {
+        const int c = 2 * j + e;
+        word(NORM_HEAD, k, c, threadIdx.x) = any_end ? heads[(k * NORM_COLS + c) * threads + threadIdx.x] : g[e];      // without an end all is `head`
+        word(NORM_TOT, k, c, threadIdx.x) = a[e];
+        word(NORM_STAT, k, c, threadIdx.x) = v[e];
+        word(NORM_TAIL, k, c, threadIdx.x) = any_end ? g[e] : 0.f;
       }
-    __syncthreads();
-    bool l_end = false;
-    for (int g = 0; g < groups; ++g) l_end |= group_end[g] != 0;
-    for (int c = threadIdx.x; c < width && col0 + c < d; c += blockDim.x) {
-      float L[NORM_PARTS] = {smem[c], smem[NORM_TOT * width + c], smem[NORM_STAT * width + c], smem[NORM_TAIL * width + c]};
-      bool le = group_end[0] != 0;
-      for (int g = 1; g < groups; ++g) {
-        const float* at = smem + (size_t)g * NORM_PARTS * width + c;
-        const bool re = group_end[g] != 0;
-        const float R[NORM_PARTS] = {at[0], at[NORM_TOT * width], at[NORM_STAT * width], at[NORM_TAIL * width]};
-        norm_join(p.phi, le, L, re, R);
-        le |= re;
-      }
-      float* out = p.parts + ((size_t)blockIdx.x * NORM_PARTS * KINDS + k) * d + col0 + c;
-#pragma unroll
-      for (int q = 0; q < NORM_PARTS; ++q) out[(size_t)q * KINDS * d] = L[q];
     }
-    if (k == 0 && threadIdx.x == 0 && (WHOLE || blockIdx.y == 0)) p.ends[blockIdx.x] = l_end;
+  if (t == 0) group_end[group] = any_end;
+  __syncthreads();
+  // The block's groups are joined, a (kind, feature of a thread, thread of a group) at a time.
+  for (int item = threadIdx.x; item < KINDS * NORM_COLS * G; item += threads) {
+    const int kc = item / G, tt = item - kc * G, k = kc / NORM_COLS, c = kc - k * NORM_COLS;
+    const int col = col0 + (c / E * G + tt) * E + c % E;
+    if (col >= d) continue;
+    float L[NORM_PARTS] = {word(0, k, c, tt), word(1, k, c, tt), word(2, k, c, tt), word(3, k, c, tt)};
+    bool le = group_end[0] != 0;
+    for (int g = 1; g < groups; ++g) {
+      const bool re = group_end[g] != 0;
+      const int th = g * G + tt;
+      const float Rr[NORM_PARTS] = {word(0, k, c, th), word(1, k, c, th), word(2, k, c, th), word(3, k, c, th)};
+      norm_join(p.phi, le, L, re, Rr);
+      le |= re;
+    }
+    float* out = p.parts + ((size_t)blockIdx.x * NORM_PARTS * KINDS + k) * d + col;
+#pragma unroll
+    for (int q = 0; q < NORM_PARTS; ++q) out[(size_t)q * KINDS * d] = L[q];
+  }
+  if (threadIdx.x == 0 && (WHOLE || blockIdx.y == 0)) {
+    int l_end = 0;
+    for (int g = 0; g < groups; ++g) l_end |= group_end[g];
+    p.ends[blockIdx.x] = l_end;
   }
 }
 
