@@ -40,15 +40,14 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
     return launch_dependent(norm_forward_wide_kernel<T, RMS>, dim3((unsigned)std::min<long long>(rows, 2ll * di->sm_count)), p.threads, 0, st, x, gain,
                             bias, rows, d, eps, y, mean, rstd);
   const int wide = aligned(gain, 16) && aligned(bias, 16);
-  // two rows at a time where enough of them remain to fill the device
-  const int groups = p.threads / p.G, r = p.G <= 32 && rows >= 64ll * di->sm_count ? 2 : 1;
-  const long long blocks = (rows + (long long)groups * r - 1) / ((long long)groups * r);
+  const int groups = p.threads / p.G;
+  const long long blocks = (rows + groups - 1) / groups;
   if (blocks >= (1ll << 31)) return PE_ERR_DIM;
   const dim3 grid((unsigned)blocks);
   auto run = [&](auto nv) {
     constexpr int NV = decltype(nv)::value;
-    if (r == 2) return launch_dependent(norm_forward_kernel<T, E, NV, 2, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
-    return launch_dependent(norm_forward_kernel<T, E, NV, 1, RMS>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
+    if (p.G <= 32) return launch_dependent(norm_forward_kernel<T, E, NV, RMS, true>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
+    return launch_dependent(norm_forward_kernel<T, E, NV, RMS, false>, grid, p.threads, 0, st, x, gain, bias, rows, d, eps, y, mean, rstd, p.G, wide);
   };
   switch (p.nv) {
     case 1: return run(std::integral_constant<int, 1>{});

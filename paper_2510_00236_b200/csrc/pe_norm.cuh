@@ -132,82 +132,95 @@ __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, 
 }
 
 // ---------------------------------------------------------------- forward
-// NV vectors of E features per thread: vector i of a thread is features (i G + thread) E ..; R rows at a time share what is loaded of gain and bias.
-// The rows stay in registers between their sums (mean first, then the squared deviations: no cancellation) and the output.
-template <typename T, int E, int NV, int R, bool RMS>
-__global__ void __launch_bounds__(R > 1 ? 256 : 512)
+// NV vectors of E features per thread: vector i of a thread is features (i G + thread) E ..
+// The row stays in registers between its sums (mean first, then the squared deviations: no cancellation) and the output.  Arithmetic is on pairs of
+// features where a vector has them, one instruction for both.  WARP: a row to at most 32 lanes; three blocks to an SM keep 96 KB of loads in flight.
+template <typename T, int E, int NV, bool RMS, bool WARP>
+__global__ void __launch_bounds__(WARP ? 256 : 512, WARP ? 3 : 1)
 norm_forward_kernel(const T* __restrict__ x, const float* __restrict__ gain, const float* __restrict__ bias, long long rows, int d, float eps,
                     T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, int G, int wide) {
-  __shared__ float slots[2 * NORM_MAX_WARPS * R];
-  sm100::griddep_launch_dependents();
-  sm100::griddep_wait();
+  using namespace sm100;
+  constexpr int W = E > 1 ? E / 2 : 1;      // pairs of a vector; a vector of one feature is a pair with a zero
+  __shared__ float slots[2 * NORM_MAX_WARPS];
+  griddep_launch_dependents();
+  griddep_wait();
   const int group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G;
-  const float inv_d = 1.f / (float)d;
   int turn = 0;
-  const long long row0 = ((long long)blockIdx.x * groups + group) * R;
-  NormVec<T, E> in[R][NV];
-#pragma unroll
-  for (int k = 0; k < R; ++k)
+  const long long row = (long long)blockIdx.x * groups + group;
+  const bool live = row < rows;
+  NormVec<T, E> in[NV];
+  {
+    const T* at = x + row * d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + t) * E;
-      if (row0 + k < rows && col < d) in[k][i].load(x + (row0 + k) * d + col);
-      else in[k][i].zero();
+      if (live && col < d) in[i].load(at + col);
+      else in[i].zero();
     }
-  float mu[R], q[R];
+  }
+  auto pairs = [&](int i, uint64_t (&o)[W]) {
+    float f[E];
+    in[i].get(f);
 #pragma unroll
-  for (int k = 0; k < R; ++k) mu[k] = q[k] = 0.f;
+    for (int j = 0; j < W; ++j) o[j] = f32x2_pack(f[E > 1 ? 2 * j : 0], E > 1 ? f[2 * j + 1] : 0.f);
+  };
+  float mu = 0.f, lo, hi;
   if constexpr (!RMS) {
+    uint64_t s2 = 0ull;
 #pragma unroll
-    for (int k = 0; k < R; ++k)
+    for (int i = 0; i < NV; ++i) {
+      uint64_t f[W];
+      pairs(i, f);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float f[E];
-        in[k][i].get(f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) mu[k] += f[e];
-      }
-    norm_group_sum<R>(mu, G, group, t, slots, turn);
-#pragma unroll
-    for (int k = 0; k < R; ++k) mu[k] = mu[k] / (float)d;      // rounded once: a row of one value keeps it
-  }
-#pragma unroll
-  for (int k = 0; k < R; ++k)
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if ((i * G + t) * E < d) {
-        float f[E];
-        in[k][i].get(f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) q[k] = fmaf(f[e] - mu[k], f[e] - mu[k], q[k]);
-      }
-  norm_group_sum<R>(q, G, group, t, slots, turn);
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    q[k] = 1.f / sqrtf(q[k] * inv_d + eps);
-    if (t == 0 && row0 + k < rows) {
-      if (!RMS && mean) mean[row0 + k] = mu[k];
-      if (rstd) rstd[row0 + k] = q[k];
+      for (int j = 0; j < W; ++j) s2 = f32x2_add(s2, f[j]);
     }
+    f32x2_unpack(s2, lo, hi);
+    float s[1] = {lo + hi};
+    norm_group_sum<1>(s, G, group, t, slots, turn);
+    mu = s[0] / (float)d;      // rounded once: a row of one value keeps it
   }
+  const uint64_t mu2 = f32x2_pack(mu, mu);
+  uint64_t q2 = 0ull;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if ((i * G + t) * E < d) {
+      uint64_t f[W];
+      pairs(i, f);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const uint64_t c = RMS ? f[j] : f32x2_sub(f[j], mu2);
+        q2 = f32x2_fma(c, c, q2);
+      }
+    }
+  f32x2_unpack(q2, lo, hi);
+  float q[1] = {E > 1 ? lo + hi : lo};
+  norm_group_sum<1>(q, G, group, t, slots, turn);
+  const float r = 1.f / sqrtf(q[0] / (float)d + eps);
+  if (!live) return;
+  if (t == 0) {
+    if (!RMS && mean) mean[row] = mu;
+    if (rstd) rstd[row] = r;
+  }
+  const uint64_t r2 = f32x2_pack(r, r);
+  T* at = y + row * d;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int col = (i * G + t) * E;
     if (col < d) {
-      float g[E], b[E];
+      float g[E], b[E], o[E];
       if (gain) norm_load_param<E>(gain, col, wide, g);
       if (bias) norm_load_param<E>(bias, col, wide, b);
+      uint64_t f[W];
+      pairs(i, f);
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        float f[E], o[E];
-        in[k][i].get(f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float h = (f[e] - mu[k]) * q[k];
-          o[e] = gain ? (bias ? fmaf(h, g[e], b[e]) : h * g[e]) : (bias ? h + b[e] : h);
-        }
-        if (row0 + k < rows) NormVec<T, E>::store(y + (row0 + k) * d + col, o);
+      for (int j = 0; j < W; ++j) {
+        uint64_t h = f32x2_mul(RMS ? f[j] : f32x2_sub(f[j], mu2), r2);
+        const uint64_t g2 = f32x2_pack(g[E > 1 ? 2 * j : 0], E > 1 ? g[2 * j + 1] : 0.f), b2 = f32x2_pack(b[E > 1 ? 2 * j : 0], E > 1 ? b[2 * j + 1] : 0.f);
+        h = gain ? (bias ? f32x2_fma(h, g2, b2) : f32x2_mul(h, g2)) : (bias ? f32x2_add(h, b2) : h);
+        if constexpr (E > 1) f32x2_unpack(h, o[2 * j], o[2 * j + 1]);
+        else f32x2_unpack(h, o[0], hi);
       }
+      NormVec<T, E>::store(at + col, o);
     }
   }
 }
@@ -366,15 +379,20 @@ __device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, i
     float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
     if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = 0.f;
-    for (int w = 0; w < warps; ++w) {
-#pragma unroll
-      for (int k = 0; k < N; k += 2) {
-        const float2 q = *reinterpret_cast<const float2*>(slot + (first + w) * N + k);
-        v[k] += q.x; v[k + 1] += q.y;
-      }
+    // a lane sums the warps' values (l mod N / 2) 2 and the one after it, of every 64 / N-th warp
+    float2 q = make_float2(0.f, 0.f);
+    for (int w = lane / (N / 2); w < warps; w += 64 / N) {
+      const float2 one = *reinterpret_cast<const float2*>(slot + (first + w) * N + (lane % (N / 2)) * 2);
+      q.x += one.x;
+      q.y += one.y;
     }
+#pragma unroll
+    for (int s2 = 16; s2 >= N / 2; s2 >>= 1) {
+      q.x += __shfl_xor_sync(0xffffffffu, q.x, s2);
+      q.y += __shfl_xor_sync(0xffffffffu, q.y, s2);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, k & 1 ? q.y : q.x, k / 2);
     turn ^= 1;
   } else {
 #pragma unroll
@@ -447,7 +465,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const long long workers = (long long)gridDim.x * groups, me = (long long)blockIdx.x * groups + group, span = last - first;
   // (span < 2^40 and workers < 2^20: the products fit)
   const long long r0 = first + span * me / workers, r1 = first + span * (me + 1) / workers;
-  const int turns = (int)((span + workers * R - 1) / (workers * R)) ;      // every group of the block takes as many
+  const int turns = (int)((span + workers * R - 1) / (workers * R));      // every group of the block takes as many
+  const int n_rows = (int)(r1 - r0);
   __syncthreads();
   // the group's first thread: rows r0 + b R .. into slot b % S
   auto issue = [&](int b) {
@@ -496,20 +515,24 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   bool any_end = false;
   NormEnds ends(p, last);
   long long end = r0 < r1 ? ends.find(r0) : last;
+  int end_row = (int)min(end - r0, (long long)INT32_MAX) - 1;      // the example's last row, counted from r0
   const float inv_d = 1.f / (float)d;
-  int turn = 0;
+  int turn = 0, sl = 0;
+  uint32_t phase = 0;
+  const uint8_t* sx = ring;
   bool waits = true;
+  const float *mean_at = RMS ? nullptr : p.mean + r0, *rstd_at = p.rstd + r0;
+  T* out = dx + r0 * d + col0;
   const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
   float mu[R], rs[R];
   float2 means[WHOLE ? 1 : R];
-  auto row_values = [&](int b, float (&m)[R], float (&r)[R], float2 (&w)[WHOLE ? 1 : R]) {
+  auto row_values = [&](int row, float (&m)[R], float (&r)[R], float2 (&w)[WHOLE ? 1 : R]) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      const long long row = r0 + (long long)b * R + k;
-      const bool live = row < r1;
-      m[k] = (!RMS && live) ? __ldg(p.mean + row) : 0.f;
-      r[k] = live ? __ldg(p.rstd + row) : 0.f;
-      if constexpr (!WHOLE) w[k] = live ? p.row_means[row] : make_float2(0.f, 0.f);
+      const bool live = row + k < n_rows;
+      m[k] = (!RMS && live) ? __ldg(mean_at + row + k) : 0.f;
+      r[k] = live ? __ldg(rstd_at + row + k) : 0.f;
+      if constexpr (!WHOLE) w[k] = live ? p.row_means[r0 + row + k] : make_float2(0.f, 0.f);
     }
   };
   row_values(0, mu, rs, means);
@@ -544,20 +567,19 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     for (int j = 0; j < P; ++j) o[j] = f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
   };
   for (int b = 0; b < turns; ++b) {
-    const long long row0 = r0 + (long long)b * R;
-    const int sl = b % S;
-    const uint8_t *const sx = ring + (size_t)sl * 2 * slot, *const sy = sx + slot;
-    if (waits && row0 < r1) waits = mbar_wait_bounded(bars + 8 * sl, (uint32_t)(b / S) & 1u, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
+    const int row0 = b * R;
+    const uint8_t* const sy = sx + slot;
+    if (waits && row0 < n_rows) waits = mbar_wait_bounded(bars + 8 * sl, phase, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
     __syncwarp();
     float s[SUMS];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (row0 + k < r1) {
+      if (row0 + k < n_rows) {
         uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
-        pairs(sx, x, row0, k, fx);
-        pairs(sy, dy, row0, k, fy);
+        pairs(sx, x, r0 + row0, k, fx);
+        pairs(sy, dy, r0 + row0, k, fy);
         const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
@@ -577,7 +599,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
           f32x2_unpack(s1, lo, hi);
           s[R + k] = lo + hi;
         }
-        if (row0 + k + 1 == end) {      // the example ends with this row
+        if (row0 + k == end_row) {      // the example ends with this row
 #pragma unroll
           for (int q = 0; q < KINDS; ++q)
 #pragma unroll
@@ -595,12 +617,13 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
             }
           any_end = true;
           end = ends.after(end);
+          end_row = (int)min(end - r0, (long long)INT32_MAX) - 1;
         }
       }
     }
     float nm[R], nr[R];
     float2 nw[WHOLE ? 1 : R];
-    row_values(b + 1, nm, nr, nw);
+    row_values(row0 + R, nm, nr, nw);
     if constexpr (WHOLE) {
       if (G > 32) norm_rows_sum<SUMS>(s, G, group, t, slots, turn);
       else norm_group_sum<SUMS>(s, G, group, t, slots, turn);
@@ -613,8 +636,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     if (dx) {
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        const long long row = row0 + k;
-        if (row < r1) {
+        if (row0 + k < n_rows) {
           float k0 = 0.f, k1;
           if constexpr (WHOLE) {
             k1 = -rs[k] * (rs[k] * (rs[k] * (s[k] * inv_d)));      // (s: sums of w c)
@@ -624,8 +646,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
             if constexpr (!RMS) k0 = -rs[k] * means[k].y;
           }
           uint64_t fx[P], fy[P];
-          pairs(sx, x, row0, k, fx);
-          pairs(sy, dy, row0, k, fy);
+          pairs(sx, x, r0 + row0, k, fx);
+          pairs(sy, dy, r0 + row0, k, fy);
           const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
           float o[NV][E];
 #pragma unroll
@@ -637,7 +659,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
             const int col = (i * G + t) * E;
-            if (col < cols) NormVec<T, E>::store(dx + row * d + col0 + col, o[i]);
+            if (col < cols) NormVec<T, E>::store(out + (long long)k * d + col, o[i]);
           }
         }
       }
@@ -648,6 +670,9 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       rs[k] = nr[k];
       if constexpr (!WHOLE) means[k] = nw[k];
     }
+    out += (long long)R * d;
+    sx += 2 * slot;
+    if (++sl == S) { sl = 0; sx = ring; phase ^= 1u; }
   }
   // The ring has been read for the last time: it holds the workers' elements now, part q, kind k, feature c of every thread.
   __syncthreads();
