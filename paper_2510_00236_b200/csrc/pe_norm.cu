@@ -111,7 +111,7 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
   p.blocks = (int)std::min(want, most);
   p.ends_at = align_up((size_t)p.blocks * NORM_PARTS * kinds * d * sizeof(float), 256);
   p.heads_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
-  p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
+  p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * (p.groups > 1 ? 1 : 3) * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
   p.bytes = p.means_at + (p.whole ? 0 : align_up((size_t)rows * sizeof(float2), 256));
   return p;
 }
@@ -139,11 +139,11 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
     return launch_dependent(kernel, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
   };
   if (p.whole)
-    return launch(norm_backward_kernel<T, E, RMS, KINDS, true>);
+    return a.rows < 32ll * a.B || p.groups > 1 ? launch(norm_backward_kernel<T, E, RMS, KINDS, true, true>) : launch(norm_backward_kernel<T, E, RMS, KINDS, true, false>);
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
                                           a, reinterpret_cast<float2*>(ws + p.means_at));
   if (rc != PE_OK) return rc;
-  return launch(norm_backward_kernel<T, E, RMS, KINDS, false>);
+  return launch(norm_backward_kernel<T, E, RMS, KINDS, false, true>);
 }
 
 template <typename T>

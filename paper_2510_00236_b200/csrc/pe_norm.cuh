@@ -302,7 +302,7 @@ struct NormBackward {
   int wide;                             // gain is 16-byte aligned
   float* parts;                         // [blocks][NORM_PARTS][kinds][d]; a block's element
   int* ends;                            // [blocks]: whether an example ends in the block's rows
-  float* heads;                         // [blocks x slabs][kinds][features of a thread][threads]: workers' heads, kept here until the rows are done
+  float* heads;                         // what the blocks' threads keep here until their rows are done (see there)
   unsigned int* dev_status;
   const float2* row_means;              // of each row: (mean(w xh), mean(w)), where a kernel before this one found them
 };
@@ -438,7 +438,9 @@ __device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, c
 }
 
 constexpr int NORM_MAX_THREADS = 512;      // 128 registers a thread: two blocks of 256 threads or one of 512 to an SM
-template <typename T, int E, bool RMS, int KINDS, bool WHOLE>
+// SHORT: many examples end, and the sums over them stay in registers; otherwise they are kept beside the heads in the workspace (L2), which costs
+// nothing where an example has 32 rows or more and leaves registers for rows that overlap.
+template <typename T, int E, bool RMS, int KINDS, bool WHOLE, bool SHORT>
 __global__ void __launch_bounds__(NORM_MAX_THREADS, 1)
 norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dx, const NormBackward p) {
   using namespace sm100;
@@ -494,7 +496,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   };
   if (t == 0)
     for (int b = 0; b < S - 1; ++b) issue(b);
-  uint64_t gain[P], run[KINDS][P], tot[KINDS][P], stat[KINDS][P];
+  uint64_t gain[P], run[KINDS][P], tot[SHORT ? KINDS : 1][SHORT ? P : 1], stat[SHORT ? KINDS : 1][SHORT ? P : 1];
   {
     float f[NV][E];
 #pragma unroll
@@ -510,8 +512,17 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
 #pragma unroll
   for (int k = 0; k < KINDS; ++k)
 #pragma unroll
-    for (int j = 0; j < P; ++j) run[k][j] = tot[k][j] = stat[k][j] = 0ull;
-  float* heads = p.heads + ((size_t)(blockIdx.y * gridDim.x + blockIdx.x) * KINDS * NORM_COLS) * threads;      // [kind][feature of a thread][thread]
+    for (int j = 0; j < P; ++j) {
+      run[k][j] = 0ull;
+      if constexpr (SHORT) tot[k][j] = stat[k][j] = 0ull;
+    }
+  // [head, then tot, stat unless SHORT][kind][feature of a thread][thread]; written by the thread that reads it
+  constexpr int KEPT = KINDS * NORM_COLS;
+  float* const heads = p.heads + ((size_t)(blockIdx.y * gridDim.x + blockIdx.x) * (SHORT ? 1 : 3) * KEPT) * threads + threadIdx.x;
+  if constexpr (!SHORT) {
+#pragma unroll 4
+    for (int k = KEPT; k < 3 * KEPT; ++k) heads[(size_t)k * threads] = 0.f;
+  }
   bool any_end = false;
   NormEnds ends(p, last);
   long long end = r0 < r1 ? ends.find(r0) : last;
@@ -524,18 +535,23 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const float *mean_at = RMS ? nullptr : p.mean + r0, *rstd_at = p.rstd + r0;
   T* out = dx + r0 * d + col0;
   const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
+  // A row's mean and rstd (and means): a lane holds those of one row of `chunk`, and of the chunk after it, so that no turn waits for them.
+  const int chunk = G < 32 ? G : 32, in_chunk = t & (chunk - 1);
+  float mu_held, rs_held, mu_next, rs_next;
+  float2 w_held = make_float2(0.f, 0.f), w_next = w_held;
+  auto row_values = [&](int row, float& m, float& r, float2& w) {
+    row += in_chunk;
+    const bool live = row < n_rows;
+    m = (!RMS && live) ? __ldg(mean_at + row) : 0.f;
+    r = live ? __ldg(rstd_at + row) : 0.f;
+    if constexpr (!WHOLE) w = live ? p.row_means[r0 + row] : make_float2(0.f, 0.f);
+  };
+  row_values(0, mu_held, rs_held, w_held);
+  row_values(chunk, mu_next, rs_next, w_next);
+  int held_end = chunk;      // rows up to here are held
   float mu[R], rs[R];
   float2 means[WHOLE ? 1 : R];
-  auto row_values = [&](int row, float (&m)[R], float (&r)[R], float2 (&w)[WHOLE ? 1 : R]) {
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const bool live = row + k < n_rows;
-      m[k] = (!RMS && live) ? __ldg(mean_at + row + k) : 0.f;
-      r[k] = live ? __ldg(rstd_at + row + k) : 0.f;
-      if constexpr (!WHOLE) w[k] = live ? p.row_means[r0 + row + k] : make_float2(0.f, 0.f);
-    }
-  };
-  row_values(0, mu, rs, means);
+  const bool active = E < 8 || t * E < cols;      // a thread with features (of vectors of less than 8, some may be out of range)
   // a thread's features of row k of the slot, as pairs
   auto pairs = [&](const uint8_t* tensor_slot, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
     const uint8_t* base;
@@ -546,9 +562,11 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * E;
+      if constexpr (E < 8) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[i][e] = 0.f;
-      if (c < cols) {
+        for (int e = 0; e < E; ++e) f[i][e] = 0.f;
+      }
+      if (E == 8 || c < cols) {
         const T* q = reinterpret_cast<const T*>(base) + c;
         if constexpr (E == 8) {
           const uint4 v = *reinterpret_cast<const uint4*>(q);
@@ -571,59 +589,90 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     const uint8_t* const sy = sx + slot;
     if (waits && row0 < n_rows) waits = mbar_wait_bounded(bars + 8 * sl, phase, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
     __syncwarp();
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (row0 + k >= held_end) {      // (block-uniform: chunk and row are)
+        mu_held = mu_next; rs_held = rs_next; w_held = w_next;
+        held_end += chunk;
+        row_values(held_end, mu_next, rs_next, w_next);
+      }
+      const int from = (row0 + k) & (chunk - 1);
+      mu[k] = RMS ? 0.f : __shfl_sync(0xffffffffu, mu_held, from, chunk);
+      rs[k] = __shfl_sync(0xffffffffu, rs_held, from, chunk);
+      if constexpr (!WHOLE) means[k] = make_float2(__shfl_sync(0xffffffffu, w_held.x, from, chunk), __shfl_sync(0xffffffffu, w_held.y, from, chunk));
+    }
     float s[SUMS];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
+    auto sums_of = [&](int k) {
+      if (!active) return;
+      uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
+      pairs(sx, x, r0 + row0, k, fx);
+      pairs(sy, dy, r0 + row0, k, fy);
+      const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      if (row0 + k < n_rows) {
-        uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
-        pairs(sx, x, r0 + row0, k, fx);
-        pairs(sy, dy, r0 + row0, k, fy);
-        const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
+      for (int j = 0; j < P; ++j) {
+        const uint64_t c = RMS ? fx[j] : f32x2_add(fx[j], m2);
+        if constexpr (WHOLE) {
+          const uint64_t w = f32x2_mul(fy[j], gain[j]);
+          s0 = f32x2_fma(w, c, s0);
+          if constexpr (!RMS) s1 = f32x2_add(s1, w);
+        }
+        run[0][j] = f32x2_fma(f32x2_mul(fy[j], r2), c, run[0][j]);
+        if constexpr (KINDS > 1) run[1][j] = f32x2_add(run[1][j], fy[j]);
+      }
+      float lo, hi;
+      f32x2_unpack(s0, lo, hi);
+      s[k] = lo + hi;
+      if constexpr (!RMS) {
+        f32x2_unpack(s1, lo, hi);
+        s[R + k] = lo + hi;
+      }
+    };
+    auto example_ends = [&] {
+      // (opaque to the compiler, which would else compute the words' addresses before the loop and keep all of them)
+      float* at = heads;
+      int step = threads;
+      asm volatile("" : "+l"(at), "+r"(step));
+#pragma unroll
+      for (int q = 0; q < KINDS; ++q)
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-          const uint64_t c = RMS ? fx[j] : f32x2_sub(fx[j], m2);
-          if constexpr (WHOLE) {
-            const uint64_t w = f32x2_mul(fy[j], gain[j]);
-            s0 = f32x2_fma(w, c, s0);
-            if constexpr (!RMS) s1 = f32x2_add(s1, w);
-          }
-          run[0][j] = f32x2_fma(f32x2_mul(fy[j], r2), c, run[0][j]);
-          if constexpr (KINDS > 1) run[1][j] = f32x2_add(run[1][j], fy[j]);
-        }
-        float lo, hi;
-        f32x2_unpack(s0, lo, hi);
-        s[k] = lo + hi;
-        if constexpr (!RMS) {
-          f32x2_unpack(s1, lo, hi);
-          s[R + k] = lo + hi;
-        }
-        if (row0 + k == end_row) {      // the example ends with this row
+          float g[2];
+          f32x2_unpack(run[q][j], g[0], g[1]);
+          if (!any_end) {
+            at[(q * NORM_COLS + 2 * j) * step] = g[0];
+            at[(q * NORM_COLS + 2 * j + 1) * step] = g[1];
+          } else if constexpr (SHORT) {
+            tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
+            stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g[0]), norm_phi(p.phi, g[1])));
+          } else {
 #pragma unroll
-          for (int q = 0; q < KINDS; ++q)
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-              float g0, g1;
-              f32x2_unpack(run[q][j], g0, g1);
-              if (!any_end) {
-                heads[(q * NORM_COLS + 2 * j) * threads + threadIdx.x] = g0;
-                heads[(q * NORM_COLS + 2 * j + 1) * threads + threadIdx.x] = g1;
-              } else {
-                tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
-                stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g0), norm_phi(p.phi, g1)));
-              }
-              run[q][j] = 0ull;
+            for (int e = 0; e < 2; ++e) {
+              at[(KEPT + q * NORM_COLS + 2 * j + e) * step] += g[e];
+              at[(2 * KEPT + q * NORM_COLS + 2 * j + e) * step] += norm_phi(p.phi, g[e]);
             }
-          any_end = true;
-          end = ends.after(end);
-          end_row = (int)min(end - r0, (long long)INT32_MAX) - 1;
+          }
+          run[q][j] = 0ull;
         }
-      }
+      any_end = true;
+      end = ends.after(end);
+      end_row = (int)min(end - r0, (long long)INT32_MAX) - 1;
+    };
+    // R whole rows of one example, without a branch between them; otherwise row by row
+    const bool full = row0 + R <= n_rows;
+    if (full && end_row >= row0 + R - 1) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) sums_of(k);
+      if (end_row == row0 + R - 1) example_ends();
+    } else {
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (row0 + k < n_rows) {
+          sums_of(k);
+          if (row0 + k == end_row) example_ends();
+        }
     }
-    float nm[R], nr[R];
-    float2 nw[WHOLE ? 1 : R];
-    row_values(row0 + R, nm, nr, nw);
     if constexpr (WHOLE) {
       if (G > 32) norm_rows_sum<SUMS>(s, G, group, t, slots, turn);
       else norm_group_sum<SUMS>(s, G, group, t, slots, turn);
@@ -633,42 +682,42 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     __syncwarp();
     // every thread of the group has left the slot before this one
     if (t == 0) issue(b + S - 1);
-    if (dx) {
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        if (row0 + k < n_rows) {
-          float k0 = 0.f, k1;
-          if constexpr (WHOLE) {
-            k1 = -rs[k] * (rs[k] * (rs[k] * (s[k] * inv_d)));      // (s: sums of w c)
-            if constexpr (!RMS) k0 = -rs[k] * (s[R + k] * inv_d);
-          } else {
-            k1 = -rs[k] * (rs[k] * means[k].x);
-            if constexpr (!RMS) k0 = -rs[k] * means[k].y;
-          }
-          uint64_t fx[P], fy[P];
-          pairs(sx, x, r0 + row0, k, fx);
-          pairs(sy, dy, r0 + row0, k, fy);
-          const uint64_t m2 = f32x2_pack(mu[k], mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
-          float o[NV][E];
-#pragma unroll
-          for (int j = 0; j < P; ++j) {
-            const uint64_t c = RMS ? fx[j] : f32x2_sub(fx[j], m2), w = f32x2_mul(fy[j], gain[j]);
-            const uint64_t v = f32x2_fma(c, k12, RMS ? f32x2_mul(w, r2) : f32x2_fma(w, r2, k02));
-            f32x2_unpack(v, o[2 * j / E][2 * j % E], o[(2 * j + 1) / E][(2 * j + 1) % E]);
-          }
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const int col = (i * G + t) * E;
-            if (col < cols) NormVec<T, E>::store(out + (long long)k * d + col, o[i]);
-          }
-        }
+    auto write_row = [&](int k) {
+      if (!active) return;
+      float k0 = 0.f, k1;
+      if constexpr (WHOLE) {
+        k1 = -rs[k] * (rs[k] * (rs[k] * (s[k] * inv_d)));      // (s: sums of w c)
+        if constexpr (!RMS) k0 = -rs[k] * (s[R + k] * inv_d);
+      } else {
+        k1 = -rs[k] * (rs[k] * means[k].x);
+        if constexpr (!RMS) k0 = -rs[k] * means[k].y;
       }
-    }
+      uint64_t fx[P], fy[P];
+      pairs(sx, x, r0 + row0, k, fx);
+      pairs(sy, dy, r0 + row0, k, fy);
+      const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
+      float o[NV][E];
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      mu[k] = nm[k];
-      rs[k] = nr[k];
-      if constexpr (!WHOLE) means[k] = nw[k];
+      for (int j = 0; j < P; ++j) {
+        const uint64_t c = RMS ? fx[j] : f32x2_add(fx[j], m2), w = f32x2_mul(fy[j], gain[j]);
+        const uint64_t v = f32x2_fma(c, k12, RMS ? f32x2_mul(w, r2) : f32x2_fma(w, r2, k02));
+        f32x2_unpack(v, o[2 * j / E][2 * j % E], o[(2 * j + 1) / E][(2 * j + 1) % E]);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int col = (i * G + t) * E;
+        if (E == 8 || col < cols) NormVec<T, E>::store(out + (long long)k * d + col, o[i]);
+      }
+    };
+    if (dx) {
+      if (full) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) write_row(k);
+      } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (row0 + k < n_rows) write_row(k);
+      }
     }
     out += (long long)R * d;
     sx += 2 * slot;
@@ -688,12 +737,20 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     for (int j = 0; j < P; ++j) {
       float g[2], a[2], v[2];
       f32x2_unpack(run[k][j], g[0], g[1]);
-      f32x2_unpack(tot[k][j], a[0], a[1]);
-      f32x2_unpack(stat[k][j], v[0], v[1]);
+      if constexpr (SHORT) {
+        f32x2_unpack(tot[k][j], a[0], a[1]);
+        f32x2_unpack(stat[k][j], v[0], v[1]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          a[e] = heads[(KEPT + k * NORM_COLS + 2 * j + e) * threads];
+          v[e] = heads[(2 * KEPT + k * NORM_COLS + 2 * j + e) * threads];
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int c = 2 * j + e;
-        word(NORM_HEAD, k, c, threadIdx.x) = any_end ? heads[(k * NORM_COLS + c) * threads + threadIdx.x] : g[e];      // without an end all is `head`
+        word(NORM_HEAD, k, c, threadIdx.x) = any_end ? heads[(k * NORM_COLS + c) * threads] : g[e];      // without an end all is `head`
         word(NORM_TOT, k, c, threadIdx.x) = a[e];
         word(NORM_STAT, k, c, threadIdx.x) = v[e];
         word(NORM_TAIL, k, c, threadIdx.x) = any_end ? g[e] : 0.f;
