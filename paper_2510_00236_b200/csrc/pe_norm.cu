@@ -1,5 +1,6 @@
 // Entry points of the normalisation layers: argument checks, the choice of the launch, and the launches.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "pe_host.cuh"
@@ -21,8 +22,8 @@ static ForwardPlan plan_forward(int d, int E) {
   } else if (vectors <= 256) {
     while (p.nv * 32 < vectors) p.nv *= 2;
   } else if (vectors <= 4096) {
-    p.nv = 8;
-    p.G = (vectors + 255) / 256 * 32;
+    p.nv = vectors <= 1024 ? 4 : 8;
+    p.G = (vectors + 32 * p.nv - 1) / (32 * p.nv) * 32;
   } else {
     p.G = 0;
     p.threads = 1024;
@@ -32,14 +33,32 @@ static ForwardPlan plan_forward(int d, int E) {
   return p;
 }
 
+// Threads to a row where each has 8 of its features: a power of two up to a warp, whole warps above.
+static int row_threads(int d) {
+  const int threads = (d + NORM_COLS - 1) / NORM_COLS;
+  if (threads > 32) return (threads + 31) / 32 * 32;
+  int G = 1;
+  while (G < threads) G *= 2;
+  return G;
+}
+
 template <typename T, int E, bool RMS>
 static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain, const float* bias, long long rows, int d, float eps, T* y,
                                   float* mean, float* rstd, cudaStream_t st) {
+  const int wide = aligned(gain, 16) && aligned(bias, 16), ring_G = row_threads(d);
+  const long long ring_min = getenv("PE_RING") ? atoll(getenv("PE_RING")) : (1ll << 21);
+  if (ring_G <= NORM_MAX_THREADS && rows * d >= ring_min) {
+    const int groups = std::max(1, 256 / ring_G), threads = ring_G * groups, smem = (int)(groups * NORM_STAGES * (norm_slot_bytes(norm_rows<T>(), d, sizeof(T), true) + 8));
+    const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 3072)));
+    const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
+    auto kernel = norm_forward_ring_kernel<T, E, RMS>;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    return launch_dependent(kernel, dim3((unsigned)blocks), threads, smem, st, x, gain, bias, rows, d, eps, y, mean, rstd, ring_G, wide, di->status_ptr);
+  }
   const ForwardPlan p = plan_forward(d, E);
   if (p.G == 0)
     return launch_dependent(norm_forward_wide_kernel<T, RMS>, dim3((unsigned)std::min<long long>(rows, 2ll * di->sm_count)), p.threads, 0, st, x, gain,
                             bias, rows, d, eps, y, mean, rstd);
-  const int wide = aligned(gain, 16) && aligned(bias, 16);
   const int groups = p.threads / p.G;
   const long long blocks = (rows + groups - 1) / groups;
   if (blocks >= (1ll << 31)) return PE_ERR_DIM;
@@ -82,45 +101,49 @@ static pe_status_t forward_impl(const T* x, const float* gain, const float* bias
 }
 
 // ---------------------------------------------------------------- backward
-constexpr int NORM_WHOLE_THREADS = NORM_MAX_THREADS;      // a block of the one-pass kernel: rows of up to 4096 features
 constexpr int NORM_SLAB_THREADS = 256;       // a block of the two-pass kernel: 2048 features
 constexpr int NORM_SM_COUNT = 148;           // the workspace is sized for launches of at most this many SMs
 struct BackwardPlan {
-  bool whole;
-  int G, groups, blocks, slabs;              // blocks along the rows; slabs of features (two-pass)
+  int mode;                                  // NORM_WHOLE up to 4096 features, NORM_CLUSTER up to 32768, NORM_SLAB
+  int G, groups, blocks, slabs;              // threads per row (of a slice), rows at a time, blocks along the rows, slices
+  bool kept;                                 // room for sums over long examples beside the heads: not for narrow rows, whose workers are many
   size_t ends_at, heads_at, means_at, bytes; // workspace: elements, their flags, heads, the rows' means
 };
 static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count) {
   BackwardPlan p = {};
   sm_count = std::min(sm_count, NORM_SM_COUNT);
-  const int threads = (d + NORM_COLS - 1) / NORM_COLS;
-  p.whole = threads <= NORM_WHOLE_THREADS;
+  p.G = row_threads(d);
   p.slabs = 1;
-  if (!p.whole) {
-    p.G = NORM_SLAB_THREADS;
-    p.slabs = (threads + p.G - 1) / p.G;
-  } else if (threads <= 32) {
-    p.G = 1;
-    while (p.G < threads) p.G *= 2;
-  } else {
-    p.G = (threads + 31) / 32 * 32;
+  if (p.G > NORM_MAX_THREADS) {
+    p.slabs = (p.G + NORM_MAX_THREADS - 1) / NORM_MAX_THREADS;
+    p.mode = NORM_CLUSTER;
+    p.G = row_threads((d + p.slabs - 1) / p.slabs);
+    if (p.slabs > NORM_MAX_CLUSTER) {
+      p.mode = NORM_SLAB;
+      p.G = NORM_SLAB_THREADS;
+      p.slabs = (d + NORM_COLS * p.G - 1) / (NORM_COLS * p.G);
+    }
   }
   p.groups = std::max(1, 256 / p.G);
+  p.kept = p.mode == NORM_CLUSTER || (p.mode == NORM_WHOLE && p.G >= 64);
   const long long want = std::max(1ll, rows / (8ll * p.groups));      // at least eight rows to a worker
-  const long long most = p.whole ? sm_count * std::max(1, 512 / (p.G * p.groups)) : std::max(1, 2 * sm_count / p.slabs);
+  const long long most = p.mode == NORM_WHOLE ? sm_count * std::max(1, 512 / (p.G * p.groups)) : std::max(1, (p.mode == NORM_SLAB ? 2 : 1) * sm_count / p.slabs);
   p.blocks = (int)std::min(want, most);
   p.ends_at = align_up((size_t)p.blocks * NORM_PARTS * kinds * d * sizeof(float), 256);
   p.heads_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
-  p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * (p.groups > 1 ? 1 : 3) * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
-  p.bytes = p.means_at + (p.whole ? 0 : align_up((size_t)rows * sizeof(float2), 256));
+  p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * (p.kept ? 3 : 1) * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
+  p.bytes = p.means_at + (p.mode == NORM_SLAB ? align_up((size_t)rows * sizeof(float2), 256) : 0);
   return p;
 }
 
+// Clusters of `size` blocks of this kernel that the device runs at a time (0: not known yet); more would wait for a second round.
+static std::atomic<int> g_clusters[MAX_DEVICES][NORM_MAX_CLUSTER + 1];
+
 template <typename T, int E, bool RMS, int KINDS>
-static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, const BackwardPlan& p, char* ws, cudaStream_t st) {
+static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, BackwardPlan& p, char* ws, cudaStream_t st) {
   const int threads = p.G * p.groups;
   // the ring and its barriers, and in the same place later the workers' elements
-  const size_t slot = norm_slot_bytes(norm_rows<T>(), p.whole ? a.d : p.G * NORM_COLS, sizeof(T), p.whole);
+  const size_t slot = norm_slot_bytes(norm_rows<T>(), p.mode == NORM_WHOLE ? a.d : p.G * NORM_COLS, sizeof(T), p.mode == NORM_WHOLE);
   const int smem = (int)std::max((size_t)p.groups * NORM_STAGES * (2 * slot + 8), (size_t)threads * NORM_PARTS * KINDS * NORM_COLS * sizeof(float));
   a.G = p.G;
   a.parts = reinterpret_cast<float*>(ws);
@@ -138,12 +161,40 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
     }
     return launch_dependent(kernel, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
   };
-  if (p.whole)
-    return a.rows < 32ll * a.B || p.groups > 1 ? launch(norm_backward_kernel<T, E, RMS, KINDS, true, true>) : launch(norm_backward_kernel<T, E, RMS, KINDS, true, false>);
+  if (p.mode == NORM_WHOLE)
+    return a.rows < 32ll * a.B || !p.kept ? launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_WHOLE, true>) : launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_WHOLE, false>);
+  if (p.mode == NORM_CLUSTER) {
+    auto kernel = norm_backward_kernel<T, E, RMS, KINDS, NORM_CLUSTER, false>;
+    const pe_status_t rc = large_smem(kernel);
+    if (rc != PE_OK) return rc;
+    a.cluster = p.slabs;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.slabs; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    int most = g_clusters[dev][p.slabs].load();
+    if (most == 0) {
+      cfg.numAttrs = 1;
+      cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
+      if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) { cudaGetLastError(); return PE_ERR_CUDA; }
+      g_clusters[dev][p.slabs].store(most);
+    }
+    p.blocks = std::min(p.blocks, most);
+    cfg.numAttrs = 2;
+    cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
+    if (cudaLaunchKernelEx(&cfg, kernel, x, dy, dx, a) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    return check_launch();
+  }
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
                                           a, reinterpret_cast<float2*>(ws + p.means_at));
   if (rc != PE_OK) return rc;
-  return launch(norm_backward_kernel<T, E, RMS, KINDS, false, true>);
+  return launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_SLAB, true>);
 }
 
 template <typename T>
@@ -171,7 +222,7 @@ static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, con
   }
   const bool bias = bias_sum || bias_stat, rms = kind == PE_NORM_RMS;
   const int kinds = bias ? 2 : 1;
-  const BackwardPlan p = plan_backward(rows, d, kinds, di->sm_count);
+  BackwardPlan p = plan_backward(rows, d, kinds, di->sm_count);
   if (!workspace || workspace_bytes < p.bytes) return PE_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return PE_ERR_ALIGN;
   NormBackward a = {};

@@ -131,6 +131,162 @@ __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, 
   }
 }
 
+// The group sum of norm_group_sum for N = 8, 4 or 2 values, by halving exchanges: 9 instead of 40 exchanges for 8 values.  Needs G >= 32.
+// `then` is applied to every sum before it goes to all lanes.
+template <int N, typename Then>
+__device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, int thread_in_group, float* slots, int& turn, Then then) {
+  const int lane = threadIdx.x & 31;
+  float a[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) a[k] = v[k];
+  int held = N, s = 16;
+#pragma unroll
+  for (int step = 0; step < 5; ++step) {
+    if (held > 1) {      // (compile-time after unrolling) the lane keeps the half of its values that its bit picks
+      const int half = held / 2;
+      const bool high = lane & s;
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k)
+        if (k < half) {
+          const float give = high ? a[k] : a[k + half], keep = high ? a[k + half] : a[k];
+          a[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
+        }
+      held = half;
+    } else {
+      a[0] += __shfl_xor_sync(0xffffffffu, a[0], s);
+    }
+    s >>= 1;
+  }
+  // lane bits 4, 3, .. pick value bits log2(N) - 1, ..
+  constexpr int SHIFT = N == 8 ? 2 : N == 4 ? 3 : 4;
+  if (G > 32) {
+    const int warps = G >> 5, first = group * warps;
+    float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
+    if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
+    __syncthreads();
+    // a lane sums the warps' values (l mod N / 2) 2 and the one after it, of every 64 / N-th warp
+    float2 q = make_float2(0.f, 0.f);
+    for (int w = lane / (N / 2); w < warps; w += 64 / N) {
+      const float2 one = *reinterpret_cast<const float2*>(slot + (first + w) * N + (lane % (N / 2)) * 2);
+      q.x += one.x;
+      q.y += one.y;
+    }
+#pragma unroll
+    for (int s2 = 16; s2 >= N / 2; s2 >>= 1) {
+      q.x += __shfl_xor_sync(0xffffffffu, q.x, s2);
+      q.y += __shfl_xor_sync(0xffffffffu, q.y, s2);
+    }
+    q.x = then(q.x);
+    q.y = then(q.y);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, k & 1 ? q.y : q.x, k / 2);
+    turn ^= 1;
+  } else {
+    a[0] = then(a[0]);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, a[0], k << SHIFT);
+  }
+}
+
+struct NormAsIs {
+  __device__ __forceinline__ float operator()(float s) const { return s; }
+};
+
+// Either way of summing, with `then`.
+template <int N, typename Then>
+__device__ __forceinline__ void norm_sums(float (&v)[N], int G, int group, int thread_in_group, float* slots, int& turn, Then then) {
+  if (G >= 32) {
+    norm_rows_sum<N>(v, G, group, thread_in_group, slots, turn, then);
+  } else {
+    norm_group_sum<N>(v, G, group, thread_in_group, slots, turn);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = then(v[k]);
+  }
+}
+
+// ---------------------------------------------------------------- rows by way of shared memory
+constexpr int NORM_COLS = 8;                     // features per thread
+constexpr int NORM_MAX_THREADS = 512;
+constexpr int NORM_STAGES = 3;
+template <typename T> __host__ __device__ constexpr int norm_rows() { return sizeof(T) == 2 ? 4 : 2; }      // R: a slot of 256 threads is 32 KB
+enum : int { NORM_WAIT_ROWS = 201 };
+
+// Bytes of a slot: R rows of one tensor and what alignment to 16 bytes adds at both ends (slab: of every row).
+__host__ __device__ constexpr size_t norm_slot_bytes(int R, int cols, int elem, bool whole) {
+  return whole ? (((size_t)R * cols * elem + 15) / 16 * 16 + 32) : (size_t)R * (((size_t)cols * elem + 15) / 16 * 16 + 32);
+}
+
+// Copies n bytes from global memory at `src` to shared memory at dst + (src & 15), dst 16-byte aligned: the 16-byte aligned part by a bulk copy
+// counted on `bar`, whose bytes are returned; begin, end: the tensor.  Only where an aligned word reaches out of the tensor its bytes are copied one element at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, const T* src, size_t n, const T* begin, const T* end, uint32_t bar, bool issue) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(src), lo0 = a & ~(uintptr_t)15, hi0 = (a + n + 15) & ~(uintptr_t)15;
+  uintptr_t lo = lo0, hi = hi0;
+  if (lo < reinterpret_cast<uintptr_t>(begin)) lo += 16;
+  if (hi > reinterpret_cast<uintptr_t>(end)) hi -= 16;
+  if (hi < lo) hi = lo;
+  if (!issue) {      // first call: the odd ends, and the number of bytes to expect
+    for (uintptr_t q = a; q < a + n && q < lo; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
+    for (uintptr_t q = hi > a ? hi : a; q < a + n; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
+    return (uint32_t)(hi - lo);
+  }
+  if (hi > lo)
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + (uint32_t)(lo - lo0)), "l"(lo),
+                 "r"((uint32_t)(hi - lo)), "r"(bar) : "memory");
+  return 0;
+}
+
+// A thread's 8 features of a row in shared memory, as pairs: its first vector is at byte `at`, the next ones G vectors further on; `fill` where a feature is
+// out of range (vectors of 8: the caller leaves such threads out).
+template <typename T, int E>
+__device__ __forceinline__ void norm_row_pairs(const uint8_t* shared, uint32_t at, int G, int t, int cols, float fill, uint64_t (&o)[NORM_COLS / 2]) {
+  constexpr int NV = NORM_COLS / E;
+  float f[NV][E];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint8_t* q = shared + (at + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)));
+    if constexpr (E == 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(q);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int h = 0; h < 4; ++h) { f[i][2 * h] = __uint_as_float(w[h] << 16); f[i][2 * h + 1] = __uint_as_float(w[h] & 0xffff0000u); }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[i][e] = fill;
+      if ((i * G + t) * E < cols) {
+        if constexpr (E == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(q);
+          f[i][0] = v.x; f[i][1] = v.y; f[i][2] = v.z; f[i][3] = v.w;
+        } else {
+          f[i][0] = (float)*reinterpret_cast<const T*>(q);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NORM_COLS / 2; ++j) o[j] = sm100::f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
+}
+
+// s / d, with a reciprocal and a correction by the remainder: the quotient itself where it is a float, so that the mean of equal values is that value.
+__device__ __forceinline__ float norm_mean(float s, float d, float inv_d) {
+  const float m = s * inv_d, rest = fmaf(-m, d, s), better = fmaf(rest, inv_d, m);
+  return better == better ? better : m;      // (an infinite sum has no remainder)
+}
+// 1 / sqrt(v) by the hardware's estimate and one Newton step for y^-2 - v = 0.
+__device__ __forceinline__ float norm_rstd(float v) {
+  const float y = rsqrtf(v), rest = fmaf(-v * y, y, 1.f), better = fmaf(0.5f * y, rest, y);
+  return better == better ? better : y;      // (v = 0 or infinite)
+}
+
+struct NormMean {
+  float d, inv_d;
+  __device__ __forceinline__ float operator()(float s) const { return norm_mean(s, d, inv_d); }
+};
+struct NormRstd {
+  float inv_d, eps;
+  __device__ __forceinline__ float operator()(float s) const { return norm_rstd(fmaf(s, inv_d, eps)); }
+};
+
 // ---------------------------------------------------------------- forward
 // NV vectors of E features per thread: vector i of a thread is features (i G + thread) E ..
 // The row stays in registers between its sums (mean first, then the squared deviations: no cancellation) and the output.  Arithmetic is on pairs of
@@ -177,7 +333,7 @@ norm_forward_kernel(const T* __restrict__ x, const float* __restrict__ gain, con
     f32x2_unpack(s2, lo, hi);
     float s[1] = {lo + hi};
     norm_group_sum<1>(s, G, group, t, slots, turn);
-    mu = s[0] / (float)d;      // rounded once: a row of one value keeps it
+    mu = norm_mean(s[0], (float)d, 1.f / (float)d);
   }
   const uint64_t mu2 = f32x2_pack(mu, mu);
   uint64_t q2 = 0ull;
@@ -195,7 +351,7 @@ norm_forward_kernel(const T* __restrict__ x, const float* __restrict__ gain, con
   f32x2_unpack(q2, lo, hi);
   float q[1] = {E > 1 ? lo + hi : lo};
   norm_group_sum<1>(q, G, group, t, slots, turn);
-  const float r = 1.f / sqrtf(q[0] / (float)d + eps);
+  const float r = norm_rstd(fmaf(q[0], 1.f / (float)d, eps));
   if (!live) return;
   if (t == 0) {
     if (!RMS && mean) mean[row] = mu;
@@ -222,6 +378,158 @@ norm_forward_kernel(const T* __restrict__ x, const float* __restrict__ gain, con
       }
       NormVec<T, E>::store(at + col, o);
     }
+  }
+}
+
+// The same for many rows: as in the backward pass below, blocks stay, a thread keeps gain and bias of its 8 features in registers, and rows come through a
+// ring of bulk copies.  (Read again for every row, gain and bias are 8 bytes per feature from L1 beside 4 from HBM: 58 % of the copy rate with bf16
+// rows, 87 % with fp32 ones.)
+template <typename T, int E, bool RMS>
+__global__ void __launch_bounds__(NORM_MAX_THREADS, E == 1 ? 1 : 2)      // (one feature at a time takes more registers)
+norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain, const float* __restrict__ bias, long long rows, int d, float eps,
+                         T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, int G, int wide, unsigned int* dev_status) {
+  using namespace sm100;
+  constexpr int NV = NORM_COLS / E, R = norm_rows<T>(), P = NORM_COLS / 2, S = NORM_STAGES;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ __align__(16) float slots[2 * (NORM_MAX_THREADS / 32) * R];
+  __shared__ int abort_flag;
+  const int group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G;
+  const size_t slot = norm_slot_bytes(R, d, sizeof(T), true);
+  uint8_t* ring = smem + (size_t)group * S * slot;
+  const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + (uint32_t)((size_t)groups * S * slot) + group * S * 8;
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (t == 0) {
+    for (int s = 0; s < S; ++s) mbar_init(bars + 8 * s, 1);
+    fence_barrier_init();
+  }
+  griddep_launch_dependents();
+  griddep_wait();
+  const long long workers = (long long)gridDim.x * groups, me = (long long)blockIdx.x * groups + group;
+  const long long r0 = rows * me / workers, r1 = rows * (me + 1) / workers;
+  const int turns = (int)((rows + workers * R - 1) / (workers * R)), n_rows = (int)(r1 - r0);
+  __syncthreads();
+  auto issue = [&](int b) {
+    const int row = b * R;
+    if (row >= n_rows) return;
+    const int n = min(R, n_rows - row), s = b % S;
+    const T* src = x + (r0 + row) * d;
+    const uint32_t bar = bars + 8 * s, dst = ring_s + (uint32_t)(s * slot);
+    const uint32_t bytes = norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, false);
+    mbar_arrive_expect_tx(bar, bytes);
+    norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, true);
+  };
+  if (t == 0)
+    for (int b = 0; b < S - 1; ++b) issue(b);
+  uint64_t g2[P], b2[P];
+  {
+    float f[NV][E], h[NV][E];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + t) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) { f[i][e] = 1.f; h[i][e] = 0.f; }
+      if (gain && col < d) norm_load_param<E>(gain, col, wide, f[i]);
+      if (bias && col < d) norm_load_param<E>(bias, col, wide, h[i]);
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      g2[j] = f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
+      b2[j] = f32x2_pack(h[2 * j / E][2 * j % E], h[(2 * j + 1) / E][(2 * j + 1) % E]);
+    }
+  }
+  const bool active = E < 8 || t * E < d;
+  const float fd = (float)d, inv_d = 1.f / fd;
+  int turn = 0, sl = 0;
+  uint32_t phase = 0;
+  bool waits = true;
+  const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
+  const uint32_t ring0 = (uint32_t)((size_t)group * S * slot) + (uint32_t)(t * E * sizeof(T)), row_bytes = (uint32_t)(d * sizeof(T));
+  uint32_t at = ring0;
+  char* out = reinterpret_cast<char*>(y + r0 * d + t * E);
+  for (int b = 0; b < turns; ++b) {
+    const int row0 = b * R;
+    if (waits && row0 < n_rows) waits = mbar_wait_bounded(bars + 8 * sl, phase, &abort_flag, dev_status, NORM_WAIT_ROWS, strict);
+    __syncwarp();
+    const uint32_t first = at + (E > 1 ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(x + (r0 + row0) * d) & 15));
+    // rows behind the last one hold what was there before: their results are not written
+    auto pairs = [&](int k, float fill, uint64_t (&o)[P]) { norm_row_pairs<T, E>(smem, first + k * row_bytes, G, t, d, fill, o); };
+    float mu[R], q[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) mu[k] = q[k] = 0.f;
+    if constexpr (!RMS) {
+      if (active) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          uint64_t f[P], s2 = 0ull;
+          pairs(k, 0.f, f);
+#pragma unroll
+          for (int j = 0; j < P; ++j) s2 = f32x2_add(s2, f[j]);
+          float lo, hi;
+          f32x2_unpack(s2, lo, hi);
+          mu[k] = lo + hi;
+        }
+      }
+      norm_sums<R>(mu, G, group, t, slots, turn, NormMean{fd, inv_d});
+    }
+    if (active) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        uint64_t f[P], s2 = 0ull;
+        pairs(k, mu[k], f);      // (features out of range: no deviation)
+        const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          const uint64_t c = RMS ? f[j] : f32x2_add(f[j], m2);
+          s2 = f32x2_fma(c, c, s2);
+        }
+        float lo, hi;
+        f32x2_unpack(s2, lo, hi);
+        q[k] = lo + hi;
+      }
+    }
+    norm_sums<R>(q, G, group, t, slots, turn, NormRstd{inv_d, eps});
+    __syncwarp();
+    if (t == 0) {
+      issue(b + S - 1);      // every thread of the group has left the slot before this one
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (row0 + k < n_rows) {
+          if (!RMS && mean) mean[r0 + row0 + k] = mu[k];
+          if (rstd) rstd[r0 + row0 + k] = q[k];
+        }
+    }
+    auto write_row = [&](int k) {
+      uint64_t f[P];
+      pairs(k, 0.f, f);
+      const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(q[k], q[k]);
+      float o[NV][E];
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const uint64_t h = f32x2_mul(RMS ? f[j] : f32x2_add(f[j], m2), r2);
+        f32x2_unpack(f32x2_fma(h, g2[j], b2[j]), o[2 * j / E][2 * j % E], o[(2 * j + 1) / E][(2 * j + 1) % E]);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (E == 8 || (i * G + t) * E < d) NormVec<T, E>::store(reinterpret_cast<T*>(out + (k * row_bytes + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)))), o[i]);
+    };
+    if (active) {
+      if (row0 + R <= n_rows) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) write_row(k);
+      } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (row0 + k < n_rows) write_row(k);
+      }
+    }
+    out += (size_t)R * row_bytes;
+    at += (uint32_t)slot;
+    if (++sl == S) { sl = 0; at = ring0; phase ^= 1u; }
+  }
+  __syncthreads();
+  if (abort_flag) {      // a wait gave up: copies in flight may still land here
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
   }
 }
 
@@ -272,7 +580,6 @@ norm_forward_wide_kernel(const T* __restrict__ x, const float* __restrict__ gain
 //     the examples that lie wholly inside, `tail`, the sum after the last end.
 // (L without an end, R): head = L.head + R.head, the rest R's.  (L with an end, R without): tail = L.tail + R.head.  Both with:
 // the example L.tail + R.head is complete and goes into tot.  No atomics: the sums' order is fixed by the launch's shape.
-constexpr int NORM_COLS = 8;                     // features per thread
 enum : int { NORM_HEAD = 0, NORM_TOT = 1, NORM_STAT = 2, NORM_TAIL = 3, NORM_PARTS = 4 };
 __device__ __forceinline__ float norm_phi(int phi, float g) {
   return phi == 1 ? g * g : phi == 2 ? (float)((g > 0.f) - (g < 0.f)) : g;
@@ -300,6 +607,7 @@ struct NormBackward {
   long long rows;                       // rows of the tensors
   int B, T, d, phi, G;                  // G threads per row
   int wide;                             // gain is 16-byte aligned
+  int cluster;                          // NORM_CLUSTER: blocks of a cluster
   float* parts;                         // [blocks][NORM_PARTS][kinds][d]; a block's element
   int* ends;                            // [blocks]: whether an example ends in the block's rows
   float* heads;                         // what the blocks' threads keep here until their rows are done (see there)
@@ -347,110 +655,35 @@ struct NormEnds {
   }
 };
 
-// The group sum of norm_group_sum for N = 8, 4 or 2 values, by halving exchanges: 9 instead of 40 exchanges for 8 values.  Needs G >= 32.
-template <int N>
-__device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, int thread_in_group, float* slots, int& turn) {
-  const int lane = threadIdx.x & 31;
-  float a[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) a[k] = v[k];
-  int held = N, s = 16;
-#pragma unroll
-  for (int step = 0; step < 5; ++step) {
-    if (held > 1) {      // (compile-time after unrolling) the lane keeps the half of its values that its bit picks
-      const int half = held / 2;
-      const bool high = lane & s;
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k)
-        if (k < half) {
-          const float give = high ? a[k] : a[k + half], keep = high ? a[k + half] : a[k];
-          a[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
-        }
-      held = half;
-    } else {
-      a[0] += __shfl_xor_sync(0xffffffffu, a[0], s);
-    }
-    s >>= 1;
-  }
-  // lane bits 4, 3, .. pick value bits log2(N) - 1, ..
-  constexpr int SHIFT = N == 8 ? 2 : N == 4 ? 3 : 4;
-  if (G > 32) {
-    const int warps = G >> 5, first = group * warps;
-    float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
-    if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
-    __syncthreads();
-    // a lane sums the warps' values (l mod N / 2) 2 and the one after it, of every 64 / N-th warp
-    float2 q = make_float2(0.f, 0.f);
-    for (int w = lane / (N / 2); w < warps; w += 64 / N) {
-      const float2 one = *reinterpret_cast<const float2*>(slot + (first + w) * N + (lane % (N / 2)) * 2);
-      q.x += one.x;
-      q.y += one.y;
-    }
-#pragma unroll
-    for (int s2 = 16; s2 >= N / 2; s2 >>= 1) {
-      q.x += __shfl_xor_sync(0xffffffffu, q.x, s2);
-      q.y += __shfl_xor_sync(0xffffffffu, q.y, s2);
-    }
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, k & 1 ? q.y : q.x, k / 2);
-    turn ^= 1;
-  } else {
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, a[0], k << SHIFT);
-  }
-}
-
-// KINDS: 1 for the gain alone, 2 with the bias.  WHOLE: a group has the whole row and finds the row's two means itself.  Otherwise
-// blockIdx.y picks the features and row_means has them.
+// KINDS: 1 for the gain alone, 2 with the bias.
+// NORM_WHOLE: a group has the whole row and finds the row's two means itself.  NORM_CLUSTER: wider rows are cut into slices for the blocks of a cluster,
+// which exchange their sums by way of each other's shared memory.  NORM_SLAB: wider still; blockIdx.y picks the features and row_means has the means.
 //
 // A worker's rows come through a ring in shared memory, NORM_STAGES slots of R rows, filled by bulk copies that the group's first thread issues two slots
 // ahead: 128 KB in flight on an SM without a register spent on them, whatever the rows' alignment.  (With the next row's loads in registers,
 // 264 MB of bf16 rows of 2048 features took 1467 us, a third of the copy rate: too little in flight.)  One barrier serves the sums of R rows, and tells that the slot
 // before has been read.  Arithmetic is on pairs of features, one instruction for both; with c = x - mu,
 //     mean(w xh) = r mean(w c),   dx = w r + c (-r^3 mean(w c)) - r mean(w),   G += (dy r) c.
-constexpr int NORM_STAGES = 3;
-template <typename T> __host__ __device__ constexpr int norm_rows() { return sizeof(T) == 2 ? 4 : 2; }      // R: a slot of 256 threads is 32 KB
-enum : int { NORM_WAIT_ROWS = 201 };
-
-// Bytes of a slot: R rows of one tensor and what alignment to 16 bytes adds at both ends (slab: of every row).
-__host__ __device__ constexpr size_t norm_slot_bytes(int R, int cols, int elem, bool whole) {
-  return whole ? (((size_t)R * cols * elem + 15) / 16 * 16 + 32) : (size_t)R * (((size_t)cols * elem + 15) / 16 * 16 + 32);
-}
-
-// Copies n bytes from global memory at `src` to shared memory at dst + (src & 15), dst 16-byte aligned: the 16-byte aligned part by a bulk copy
-// counted on `bar`, whose bytes are returned; begin, end: the tensor.  Only where an aligned word reaches out of the tensor its bytes are copied one element at a time.
-template <typename T>
-__device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, const T* src, size_t n, const T* begin, const T* end, uint32_t bar, bool issue) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(src), lo0 = a & ~(uintptr_t)15, hi0 = (a + n + 15) & ~(uintptr_t)15;
-  uintptr_t lo = lo0, hi = hi0;
-  if (lo < reinterpret_cast<uintptr_t>(begin)) lo += 16;
-  if (hi > reinterpret_cast<uintptr_t>(end)) hi -= 16;
-  if (hi < lo) hi = lo;
-  if (!issue) {      // first call: the odd ends, and the number of bytes to expect
-    for (uintptr_t q = a; q < a + n && q < lo; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
-    for (uintptr_t q = hi > a ? hi : a; q < a + n; q += sizeof(T)) *reinterpret_cast<T*>(dst_gen + (q - lo0)) = *reinterpret_cast<const T*>(q);
-    return (uint32_t)(hi - lo);
-  }
-  if (hi > lo)
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + (uint32_t)(lo - lo0)), "l"(lo),
-                 "r"((uint32_t)(hi - lo)), "r"(bar) : "memory");
-  return 0;
-}
-
-constexpr int NORM_MAX_THREADS = 512;      // 128 registers a thread: two blocks of 256 threads or one of 512 to an SM
 // SHORT: many examples end, and the sums over them stay in registers; otherwise they are kept beside the heads in the workspace (L2), which costs
 // nothing where an example has 32 rows or more and leaves registers for rows that overlap.
-template <typename T, int E, bool RMS, int KINDS, bool WHOLE, bool SHORT>
+enum : int { NORM_WHOLE = 0, NORM_CLUSTER = 1, NORM_SLAB = 2 };
+constexpr int NORM_MAX_CLUSTER = 8;
+template <typename T, int E, bool RMS, int KINDS, int MODE, bool SHORT>
 __global__ void __launch_bounds__(NORM_MAX_THREADS, 1)
 norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dx, const NormBackward p) {
   using namespace sm100;
   constexpr int NV = NORM_COLS / E, R = norm_rows<T>(), P = NORM_COLS / 2, SUMS = RMS ? R : 2 * R, S = NORM_STAGES;
+  constexpr bool WHOLE = MODE == NORM_WHOLE;      // (rows come in one piece)
+  constexpr bool SUMMED = MODE != NORM_SLAB;      // the means are found here
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float slots[2 * (NORM_MAX_THREADS / 32) * SUMS];
   __shared__ int group_end[256];
   __shared__ int abort_flag;
+  __shared__ float exchanged[MODE == NORM_CLUSTER ? 2 : 1][MODE == NORM_CLUSTER ? NORM_MAX_CLUSTER : 1][SUMS];
   const int G = p.G, d = p.d, group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G, threads = blockDim.x;
-  const int col0 = WHOLE ? 0 : blockIdx.y * G * NORM_COLS, cols = WHOLE ? d : min(d - col0, G * NORM_COLS);
+  const int rank = MODE == NORM_CLUSTER ? (int)cluster_ctarank() : 0, block = MODE == NORM_CLUSTER ? (int)blockIdx.x / p.cluster : (int)blockIdx.x;
+  const int blocks = MODE == NORM_CLUSTER ? (int)gridDim.x / p.cluster : (int)gridDim.x;
+  const int col0 = WHOLE ? 0 : (MODE == NORM_CLUSTER ? rank : (int)blockIdx.y) * G * NORM_COLS, cols = WHOLE ? d : max(0, min(d - col0, G * NORM_COLS));
   const size_t slot = norm_slot_bytes(R, WHOLE ? d : G * NORM_COLS, sizeof(T), WHOLE);
   // [group][stage][x, dy], then a barrier per group and stage
   uint8_t* ring = smem + (size_t)group * S * 2 * slot;
@@ -464,12 +697,13 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   griddep_wait();
   long long first, last;
   norm_span(p, first, last);
-  const long long workers = (long long)gridDim.x * groups, me = (long long)blockIdx.x * groups + group, span = last - first;
+  const long long workers = (long long)blocks * groups, me = (long long)block * groups + group, span = last - first;
   // (span < 2^40 and workers < 2^20: the products fit)
   const long long r0 = first + span * me / workers, r1 = first + span * (me + 1) / workers;
   const int turns = (int)((span + workers * R - 1) / (workers * R));      // every group of the block takes as many
   const int n_rows = (int)(r1 - r0);
-  __syncthreads();
+  if constexpr (MODE == NORM_CLUSTER) cluster_sync_all();      // every block of the cluster runs before one writes to it
+  else __syncthreads();
   // the group's first thread: rows r0 + b R .. into slot b % S
   auto issue = [&](int b) {
     const long long row = r0 + (long long)b * R;
@@ -518,7 +752,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
   // [head, then tot, stat unless SHORT][kind][feature of a thread][thread]; written by the thread that reads it
   constexpr int KEPT = KINDS * NORM_COLS;
-  float* const heads = p.heads + ((size_t)(blockIdx.y * gridDim.x + blockIdx.x) * (SHORT ? 1 : 3) * KEPT) * threads + threadIdx.x;
+  float* const heads = p.heads + ((size_t)((MODE == NORM_CLUSTER ? rank : (int)blockIdx.y) * blocks + block) * (SHORT ? 1 : 3) * KEPT) * threads + threadIdx.x;
   if constexpr (!SHORT) {
 #pragma unroll 4
     for (int k = KEPT; k < 3 * KEPT; ++k) heads[(size_t)k * threads] = 0.f;
@@ -530,10 +764,12 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const float inv_d = 1.f / (float)d;
   int turn = 0, sl = 0;
   uint32_t phase = 0;
-  const uint8_t* sx = ring;
+  const uint32_t ring0 = (uint32_t)((size_t)group * S * 2 * slot) + (uint32_t)(t * E * sizeof(T));      // this thread's first vector of slot 0
+  const uint32_t row_bytes = WHOLE ? (uint32_t)(d * sizeof(T)) : (uint32_t)(slot / R), out_bytes = (uint32_t)(d * sizeof(T));
+  uint32_t at = ring0;
   bool waits = true;
   const float *mean_at = RMS ? nullptr : p.mean + r0, *rstd_at = p.rstd + r0;
-  T* out = dx + r0 * d + col0;
+  char* out = reinterpret_cast<char*>(dx + r0 * d + col0 + t * E);
   const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
   // A row's mean and rstd (and means): a lane holds those of one row of `chunk`, and of the chunk after it, so that no turn waits for them.
   const int chunk = G < 32 ? G : 32, in_chunk = t & (chunk - 1);
@@ -544,54 +780,27 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     const bool live = row < n_rows;
     m = (!RMS && live) ? __ldg(mean_at + row) : 0.f;
     r = live ? __ldg(rstd_at + row) : 0.f;
-    if constexpr (!WHOLE) w = live ? p.row_means[r0 + row] : make_float2(0.f, 0.f);
+    if constexpr (!SUMMED) w = live ? p.row_means[r0 + row] : make_float2(0.f, 0.f);
   };
   row_values(0, mu_held, rs_held, w_held);
   row_values(chunk, mu_next, rs_next, w_next);
   int held_end = chunk;      // rows up to here are held
   float mu[R], rs[R];
-  float2 means[WHOLE ? 1 : R];
+  float2 means[SUMMED ? 1 : R];
   const bool active = E < 8 || t * E < cols;      // a thread with features (of vectors of less than 8, some may be out of range)
-  // a thread's features of row k of the slot, as pairs
-  auto pairs = [&](const uint8_t* tensor_slot, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
-    const uint8_t* base;
-    if constexpr (E > 1) base = tensor_slot + (WHOLE ? (size_t)k * d * sizeof(T) : (size_t)k * (slot / R));
-    else if constexpr (WHOLE) base = tensor_slot + (reinterpret_cast<uintptr_t>(tensor + row * d) & 15) + (size_t)k * d * sizeof(T);
-    else base = tensor_slot + (size_t)k * (slot / R) + (reinterpret_cast<uintptr_t>(tensor + (row + k) * d + col0) & 15);
-    float f[NV][E];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * G + t) * E;
-      if constexpr (E < 8) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[i][e] = 0.f;
-      }
-      if (E == 8 || c < cols) {
-        const T* q = reinterpret_cast<const T*>(base) + c;
-        if constexpr (E == 8) {
-          const uint4 v = *reinterpret_cast<const uint4*>(q);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int h = 0; h < 4; ++h) { f[i][2 * h] = __uint_as_float(w[h] << 16); f[i][2 * h + 1] = __uint_as_float(w[h] & 0xffff0000u); }
-        } else if constexpr (E == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(q);
-          f[i][0] = v.x; f[i][1] = v.y; f[i][2] = v.z; f[i][3] = v.w;
-        } else {
-          f[i][0] = (float)*q;
-        }
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < P; ++j) o[j] = f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
+  // this thread's features of row k of the slot, as pairs
+  auto pairs = [&](uint32_t tensor_at, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
+    if constexpr (E == 1) tensor_at += (uint32_t)(reinterpret_cast<uintptr_t>(tensor + (WHOLE ? row : row + k) * d + col0) & 15);
+    norm_row_pairs<T, E>(smem, tensor_at + k * row_bytes, G, t, cols, 0.f, o);
   };
   for (int b = 0; b < turns; ++b) {
     const int row0 = b * R;
-    const uint8_t* const sy = sx + slot;
+    const uint32_t at_y = at + (uint32_t)slot;
     if (waits && row0 < n_rows) waits = mbar_wait_bounded(bars + 8 * sl, phase, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (row0 + k >= held_end) {      // (block-uniform: chunk and row are)
+      if ((k == 0 || G < R) && row0 + k >= held_end) {      // (block-uniform; chunks of at least R rows end with a turn)
         mu_held = mu_next; rs_held = rs_next; w_held = w_next;
         held_end += chunk;
         row_values(held_end, mu_next, rs_next, w_next);
@@ -599,21 +808,20 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       const int from = (row0 + k) & (chunk - 1);
       mu[k] = RMS ? 0.f : __shfl_sync(0xffffffffu, mu_held, from, chunk);
       rs[k] = __shfl_sync(0xffffffffu, rs_held, from, chunk);
-      if constexpr (!WHOLE) means[k] = make_float2(__shfl_sync(0xffffffffu, w_held.x, from, chunk), __shfl_sync(0xffffffffu, w_held.y, from, chunk));
+      if constexpr (!SUMMED) means[k] = make_float2(__shfl_sync(0xffffffffu, w_held.x, from, chunk), __shfl_sync(0xffffffffu, w_held.y, from, chunk));
     }
     float s[SUMS];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
     auto sums_of = [&](int k) {
-      if (!active) return;
       uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
-      pairs(sx, x, r0 + row0, k, fx);
-      pairs(sy, dy, r0 + row0, k, fy);
+      pairs(at, x, r0 + row0, k, fx);
+      pairs(at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const uint64_t c = RMS ? fx[j] : f32x2_add(fx[j], m2);
-        if constexpr (WHOLE) {
+        if constexpr (SUMMED) {
           const uint64_t w = f32x2_mul(fy[j], gain[j]);
           s0 = f32x2_fma(w, c, s0);
           if constexpr (!RMS) s1 = f32x2_add(s1, w);
@@ -645,7 +853,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
             at[(q * NORM_COLS + 2 * j + 1) * step] = g[1];
           } else if constexpr (SHORT) {
             tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
-            stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g[0]), norm_phi(p.phi, g[1])));
+            if (p.phi == 1) stat[q][j] = f32x2_fma(run[q][j], run[q][j], stat[q][j]);
+            else stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g[0]), norm_phi(p.phi, g[1])));
           } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -662,20 +871,35 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     // R whole rows of one example, without a branch between them; otherwise row by row
     const bool full = row0 + R <= n_rows;
     if (full && end_row >= row0 + R - 1) {
+      if (active) {
 #pragma unroll
-      for (int k = 0; k < R; ++k) sums_of(k);
+        for (int k = 0; k < R; ++k) sums_of(k);
+      }
       if (end_row == row0 + R - 1) example_ends();
     } else {
 #pragma unroll
       for (int k = 0; k < R; ++k)
         if (row0 + k < n_rows) {
-          sums_of(k);
+          if (active) sums_of(k);
           if (row0 + k == end_row) example_ends();
         }
     }
-    if constexpr (WHOLE) {
-      if (G > 32) norm_rows_sum<SUMS>(s, G, group, t, slots, turn);
-      else norm_group_sum<SUMS>(s, G, group, t, slots, turn);
+    if constexpr (SUMMED) {
+      norm_sums<SUMS>(s, G, group, t, slots, turn, NormAsIs{});
+      if constexpr (MODE == NORM_CLUSTER) {      // (a turn's words are written again two turns later, with a barrier of the cluster in between)
+        if ((int)threadIdx.x < p.cluster) {
+          const uint32_t to = map_to_cta(smem_u32(&exchanged[b & 1][rank][0]), threadIdx.x);
+#pragma unroll
+          for (int k = 0; k < SUMS; ++k) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * k), "f"(s[k]) : "memory");
+        }
+        __syncwarp();
+        cluster_sync_all();
+#pragma unroll
+        for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
+        for (int q = 0; q < p.cluster; ++q)
+#pragma unroll
+          for (int k = 0; k < SUMS; ++k) s[k] += exchanged[b & 1][q][k];
+      }
     } else {
       __syncthreads();
     }
@@ -683,9 +907,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     // every thread of the group has left the slot before this one
     if (t == 0) issue(b + S - 1);
     auto write_row = [&](int k) {
-      if (!active) return;
       float k0 = 0.f, k1;
-      if constexpr (WHOLE) {
+      if constexpr (SUMMED) {
         k1 = -rs[k] * (rs[k] * (rs[k] * (s[k] * inv_d)));      // (s: sums of w c)
         if constexpr (!RMS) k0 = -rs[k] * (s[R + k] * inv_d);
       } else {
@@ -693,8 +916,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
         if constexpr (!RMS) k0 = -rs[k] * means[k].y;
       }
       uint64_t fx[P], fy[P];
-      pairs(sx, x, r0 + row0, k, fx);
-      pairs(sy, dy, r0 + row0, k, fy);
+      pairs(at, x, r0 + row0, k, fx);
+      pairs(at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
       float o[NV][E];
 #pragma unroll
@@ -704,12 +927,10 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
         f32x2_unpack(v, o[2 * j / E][2 * j % E], o[(2 * j + 1) / E][(2 * j + 1) % E]);
       }
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int col = (i * G + t) * E;
-        if (E == 8 || col < cols) NormVec<T, E>::store(out + (long long)k * d + col, o[i]);
-      }
+      for (int i = 0; i < NV; ++i)
+        if (E == 8 || (i * G + t) * E < cols) NormVec<T, E>::store(reinterpret_cast<T*>(out + (k * out_bytes + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)))), o[i]);
     };
-    if (dx) {
+    if (dx && active) {
       if (full) {
 #pragma unroll
         for (int k = 0; k < R; ++k) write_row(k);
@@ -719,9 +940,9 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
           if (row0 + k < n_rows) write_row(k);
       }
     }
-    out += (long long)R * d;
-    sx += 2 * slot;
-    if (++sl == S) { sl = 0; sx = ring; phase ^= 1u; }
+    out += (size_t)R * out_bytes;
+    at += 2 * (uint32_t)slot;
+    if (++sl == S) { sl = 0; at = ring0; phase ^= 1u; }
   }
   // The ring has been read for the last time: it holds the workers' elements now, part q, kind k, feature c of every thread.
   __syncthreads();
@@ -772,15 +993,16 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       norm_join(p.phi, le, L, re, Rr);
       le |= re;
     }
-    float* out = p.parts + ((size_t)blockIdx.x * NORM_PARTS * KINDS + k) * d + col;
+    float* out = p.parts + ((size_t)block * NORM_PARTS * KINDS + k) * d + col;
 #pragma unroll
     for (int q = 0; q < NORM_PARTS; ++q) out[(size_t)q * KINDS * d] = L[q];
   }
-  if (threadIdx.x == 0 && (WHOLE || blockIdx.y == 0)) {
+  if (threadIdx.x == 0 && rank == 0 && blockIdx.y == 0) {
     int l_end = 0;
     for (int g = 0; g < groups; ++g) l_end |= group_end[g];
-    p.ends[blockIdx.x] = l_end;
+    p.ends[block] = l_end;
   }
+  if constexpr (MODE == NORM_CLUSTER) cluster_sync_all();      // nobody leaves while its shared memory may be written
 }
 
 // The two means of every row, for rows wider than a block of norm_backward_kernel: a block per row.
@@ -808,7 +1030,7 @@ norm_row_means_kernel(const T* __restrict__ x, const T* __restrict__ dy, const N
 }
 
 // Joins the blocks' elements, in their order: a block per 32 features, its warps take consecutive elements and are joined in turn.
-constexpr int NORM_JOIN_WARPS = 16;
+constexpr int NORM_JOIN_WARPS = 32, NORM_JOIN_BATCH = 4;      // elements whose words a warp has in flight
 template <int KINDS>
 __global__ void __launch_bounds__(32 * NORM_JOIN_WARPS)
 norm_join_kernel(const float* __restrict__ parts, const int* __restrict__ ends, int blocks, int d, int phi, int accumulate,
@@ -822,14 +1044,22 @@ norm_join_kernel(const float* __restrict__ parts, const int* __restrict__ ends, 
   const int b0 = (int)((long long)blocks * warp / NORM_JOIN_WARPS), b1 = (int)((long long)blocks * (warp + 1) / NORM_JOIN_WARPS);
   float L[NORM_PARTS] = {0.f, 0.f, 0.f, 0.f};      // no rows: an element without an end
   bool le = false;
-  for (int b = b0; b < b1; ++b) {
-    const bool re = ends[b] != 0;
-    float R[NORM_PARTS];
-    const float* at = parts + ((size_t)b * NORM_PARTS * KINDS + kind) * d + col;
+  for (int b = b0; b < b1; b += NORM_JOIN_BATCH) {
+    float R[NORM_JOIN_BATCH][NORM_PARTS];
+    int re[NORM_JOIN_BATCH];
 #pragma unroll
-    for (int q = 0; q < NORM_PARTS; ++q) R[q] = col < d ? at[(size_t)q * KINDS * d] : 0.f;
-    norm_join(phi, le, L, re, R);
-    le |= re;
+    for (int k = 0; k < NORM_JOIN_BATCH; ++k) {
+      const bool live = b + k < b1;
+      const float* at = parts + ((size_t)(b + k) * NORM_PARTS * KINDS + kind) * d + col;
+      re[k] = live ? ends[b + k] : 0;
+#pragma unroll
+      for (int q = 0; q < NORM_PARTS; ++q) R[k][q] = live && col < d ? at[(size_t)q * KINDS * d] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < NORM_JOIN_BATCH; ++k) {      // (behind the last: nothing is added)
+      norm_join(phi, le, L, re[k] != 0, R[k]);
+      le |= re[k] != 0;
+    }
   }
 #pragma unroll
   for (int q = 0; q < NORM_PARTS; ++q) joined[warp][q][lane] = L[q];

@@ -1,0 +1,64 @@
+"""Rows of several thousand features: slices of a row in the blocks of a cluster, and rows too wide for that; long examples and short ones."""
+import pytest
+import torch
+
+import paper_2510_00236_b200 as pe
+from test_gpu_norm import DEV, DT, EPS, _check_backward, _rows, _stats
+from norm_reference import assert_within, forward, half_step
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,T,d", [(3, 70, 5000), (2, 40, 8192), (40, 1, 8200), (1, 33, 16384), (3, 5, 24003), (2, 7, 32768), (2, 5, 32776), (2, 3, 40001), (3, 2, 65536)])
+def test_backward_of_wide_rows(B, T, d, dtype, kind):
+    x, dy, gain, _ = _rows(B, T, d, DT[dtype], d + B)
+    mean, rstd = _stats(x, kind)
+    got = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind)
+    _check_backward(got, x, dy, gain, mean, rstd, list(range(0, B * T + 1, T)), "square", kind)
+    again = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind)
+    assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+
+
+@pytest.mark.parametrize("phi", ["square", "sign", "identity"])
+@pytest.mark.parametrize("B,T,d", [(40, 100, 2048), (9, 1000, 512), (3, 3001, 1024), (700, 33, 320), (2000, 1, 2048), (900, 2, 4096), (37, 129, 1000), (50, 64, 3001)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_backward_of_many_rows(B, T, d, phi, dtype):
+    """Every worker has several turns, examples that end inside them, at their borders and in none."""
+    x, dy, gain, _ = _rows(B, T, d, DT[dtype], d + T)
+    mean, rstd = _stats(x, "layer")
+    got = pe.pe_norm_backward(x, dy, gain, mean, rstd, phi)
+    _check_backward(got, x, dy, gain, mean, rstd, list(range(0, B * T + 1, T)), phi, "layer")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("rows,d", [(40001, 64), (9000, 512), (3001, 2048), (5003, 1001), (1700, 4096), (1500, 3333), (100003, 24), (2500, 1536)])
+def test_forward_of_many_rows(rows, d, dtype, kind):
+    x, _, gain, bias = _rows(1, rows, d, DT[dtype], rows)
+    for gn, bs in ((gain, bias), (None, None)):
+        y, mean, rstd = pe.pe_norm_forward(x, gn, bs, kind=kind, eps=EPS)
+        ry, rm, rr, y_off, m_off, r_off = forward(x.double(), gn, bs, kind, EPS)
+        assert_within("y", y, ry, y_off, half_step(DT[dtype]))
+        assert_within("rstd", rstd, rr, r_off)
+        if mean is not None:
+            assert_within("mean", mean, rm, m_off)
+
+
+def test_rows_at_the_ends_of_a_buffer():
+    """Tensors that begin and end inside a 16-byte word: the words around them stay as they were, and theirs is all that counts."""
+    B, T, d = 5, 7, 333
+    x, dy, gain, bias = _rows(B, T, d, torch.float32, 3)
+    n = x.numel()
+    for shift in (1, 2, 3):
+        store = [torch.full((n + 8,), float("nan"), device=DEV) for _ in range(4)]
+        views = [t[shift:shift + n].view(B, T, d) for t in store]
+        views[0].copy_(x)
+        views[1].copy_(dy)
+        mean, rstd = _stats(x, "layer")
+        got = pe.pe_norm_backward(views[0], views[1], gain, mean, rstd, "square", dx=views[2])
+        _check_backward(got, x, dy, gain, mean, rstd, list(range(0, B * T + 1, T)), "square", "layer")
+        pe.pe_norm_forward(views[0], gain, bias, out=views[3])
+        for t in store:
+            assert torch.isnan(t[:shift]).all() and torch.isnan(t[shift + n:]).all() and not torch.isnan(t[shift:shift + n]).any()
