@@ -554,40 +554,51 @@ def _norm_kind(kind) -> int:
     return _NORM_NAMES[kind] if isinstance(kind, str) else int(kind)
 
 
+_ROW_TYPES = (torch.bfloat16, torch.float32)
+
+
 def _float_rows(name, t, shape, device):
-    if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != device):
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on the inputs' device")
+    return t.data_ptr()
 
 
-def _norm_input(name, t, shape=None, dtype=None, device=None):
-    """Rows of d features (the last dimension), contiguous, bfloat16 or float32."""
-    if t.dtype not in (torch.bfloat16, torch.float32) or (dtype is not None and t.dtype != dtype):
+def _norm_input(name, t, shape, dtype, device):
+    """Rows of d features (the last dimension), contiguous, of x's type, shape and device."""
+    if t.dtype is not dtype or dtype not in _ROW_TYPES:
         raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, all of them the same")
-    if t.dim() < 1 or not t.is_contiguous() or (shape is not None and t.shape != shape) or (device is not None and t.device != device):
+    if t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be contiguous, of x's shape and on its device")
+    return t.data_ptr()
 
 
 def pe_norm_forward(x, gain=None, bias=None, *, kind="layer", eps=1e-5, out=None, mean=None, rstd=None):
     """y = (x - mean) * rstd * gain + bias over the last dimension of x (bf16 or float32, contiguous); kind "layer" or "rms" (mean = 0).
     gain, bias: float32 [d] or None.  Returns (y, mean, rstd); mean and rstd, float32 of x's leading shape, are what pe_norm_backward reads
     (mean is None for "rms").  Missing outputs are allocated."""
-    _norm_input("x", x)
-    lead, d, code = x.shape[:-1], x.shape[-1], _norm_kind(kind)
-    _float_rows("gain", gain, (d,), x.device)
-    _float_rows("bias", bias, (d,), x.device)
+    shape, dtype, dev, code = x.shape, x.dtype, x.device, _norm_kind(kind)
+    xp = _norm_input("x", x, shape, dtype, dev)
+    lead, d = shape[:-1], shape[-1]
+    gp = None if gain is None else _float_rows("gain", gain, (d,), dev)
+    bp = None if bias is None else _float_rows("bias", bias, (d,), dev)
     if out is None:
         out = torch.empty_like(x)
-    _norm_input("out", out, x.shape, x.dtype, x.device)
+        op = out.data_ptr()
+    else:
+        op = _norm_input("out", out, shape, dtype, dev)
     if rstd is None:
         rstd = x.new_empty(lead, dtype=torch.float32)
+        rp = rstd.data_ptr()
+    else:
+        rp = _float_rows("rstd", rstd, lead, dev)
     if code == NORM_RMS:
-        mean = None
+        mean = mp = None
     elif mean is None:
-        mean = x.new_empty(lead, dtype=torch.float32)
-    _float_rows("mean", mean, lead, x.device)
-    _float_rows("rstd", rstd, lead, x.device)
-    _launch("pe_norm_forward" if x.dtype == torch.bfloat16 else "pe_norm_forward_f32", x, x.data_ptr(), _ptr(gain), _ptr(bias), x.numel() // d if d else 0, d,
-            code, float(eps), out.data_ptr(), _ptr(mean), rstd.data_ptr())
+        mean = torch.empty_like(rstd)
+        mp = mean.data_ptr()
+    else:
+        mp = _float_rows("mean", mean, lead, dev)
+    _launch("pe_norm_forward" if dtype is torch.bfloat16 else "pe_norm_forward_f32", x, xp, gp, bp, rstd.numel(), d, code, eps, op, mp, rp)
     return out, mean, rstd
 
 
@@ -603,39 +614,50 @@ def pe_norm_backward_workspace_bytes(rows, d) -> int:
 
 
 def _norm_backward(x, dy, gain, mean, rstd, seq_offsets, phi, kind, dx, gain_sum, gain_stat, bias_sum, bias_stat, accumulate, workspace):
-    _norm_input("x", x)
-    _norm_input("dy", dy, x.shape, x.dtype, x.device)
-    code, d, lead = _norm_kind(kind), x.shape[-1], x.shape[:-1]
+    shape, dtype, dev, code = x.shape, x.dtype, x.device, _norm_kind(kind)
+    lead, d = shape[:-1], shape[-1]
+    xp = _norm_input("x", x, shape, dtype, dev)
+    yp = _norm_input("dy", dy, shape, dtype, dev)
     if dx is None:
         dx = torch.empty_like(x) if seq_offsets is None else torch.zeros_like(x)      # rows of no sequence: the library leaves them alone
-    _norm_input("dx", dx, x.shape, x.dtype, x.device)
-    if x.numel() and dx.data_ptr() in (x.data_ptr(), dy.data_ptr()):
-        raise ValueError("dx must not overlap x or dy")
-    _float_rows("gain", gain, (d,), x.device)
+        dp = dx.data_ptr()
+    else:
+        dp = _norm_input("dx", dx, shape, dtype, dev)
+        if dp and (dp == xp or dp == yp):
+            raise ValueError("dx must not overlap x or dy")
+    gp = None if gain is None else _float_rows("gain", gain, (d,), dev)
     if code == NORM_RMS:
-        mean = None
+        mp = None
     elif mean is None:
         raise ValueError("mean is required for a layer norm")
-    _float_rows("mean", mean, lead, x.device)
-    _float_rows("rstd", rstd, lead, x.device)
-    sums = [gain_sum, gain_stat, bias_sum, bias_stat]
-    if all(t is None for t in sums):
+    else:
+        mp = _float_rows("mean", mean, lead, dev)
+    rp = _float_rows("rstd", rstd, lead, dev)
+    if gain_sum is None and gain_stat is None and bias_sum is None and bias_stat is None:
         if accumulate:
             raise ValueError("accumulate needs the sums to add to")
-        sums = [x.new_empty((d,), dtype=torch.float32) for _ in range(2 if code == NORM_RMS else 4)] + [None] * (2 if code == NORM_RMS else 0)
-    for name, t in zip(("gain_sum", "gain_stat", "bias_sum", "bias_stat"), sums):
-        _float_rows(name, t, (d,), x.device)
+        both = x.new_empty((2 if code == NORM_RMS else 4, d), dtype=torch.float32)
+        at, step = both.data_ptr(), 4 * d
+        sums = both.unbind()
+        ptrs = (at, at + step, at + 2 * step, at + 3 * step) if code != NORM_RMS else (at, at + step, None, None)
+        if code == NORM_RMS:
+            sums += (None, None)
+    else:
+        sums = (gain_sum, gain_stat, bias_sum, bias_stat)
+        ptrs = [None if t is None else _float_rows(name, t, (d,), dev) for name, t in zip(("gain_sum", "gain_stat", "bias_sum", "bias_stat"), sums)]
     rows = rstd.numel()
     if workspace is None:
-        workspace = x.new_empty((pe_norm_backward_workspace_bytes(rows, d),), dtype=torch.uint8)
-    elif workspace.device != x.device or not workspace.is_contiguous():
+        ws_bytes = pe_norm_backward_workspace_bytes(rows, d)
+        workspace = x.new_empty((ws_bytes,), dtype=torch.uint8)
+    elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on x's device")
-    tail = (d, code, _phi(phi), int(bool(accumulate)), dx.data_ptr(), *map(_ptr, sums), workspace.data_ptr() or None, workspace.numel() * workspace.element_size())
-    head = (x.data_ptr(), dy.data_ptr(), _ptr(gain), _ptr(mean), rstd.data_ptr())
-    if seq_offsets is not None:
-        _launch("pe_norm_backward_ragged", x, *head, seq_offsets.data_ptr(), seq_offsets.numel() - 1, rows, *tail)
     else:
-        _launch("pe_norm_backward" if x.dtype == torch.bfloat16 else "pe_norm_backward_f32", x, *head, x.shape[0], x.shape[1], *tail)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    tail = (d, code, _phi(phi), 1 if accumulate else 0, dp, *ptrs, workspace.data_ptr() or None, ws_bytes)
+    if seq_offsets is not None:
+        _launch("pe_norm_backward_ragged", x, xp, yp, gp, mp, rp, seq_offsets.data_ptr(), seq_offsets.numel() - 1, rows, *tail)
+    else:
+        _launch("pe_norm_backward" if dtype is torch.bfloat16 else "pe_norm_backward_f32", x, xp, yp, gp, mp, rp, shape[0], shape[1], *tail)
     return (dx, *sums)
 
 

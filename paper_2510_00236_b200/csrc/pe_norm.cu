@@ -8,6 +8,20 @@
 
 namespace pe {
 
+// Lets `kernel` use `smem` bytes of shared memory on the current device; asked of the driver once per kernel, device and largest size so far.
+template <typename Kernel>
+static pe_status_t allow_smem(Kernel kernel, std::atomic<int> (&allowed)[MAX_DEVICES], int smem) {
+  if (smem <= 48 * 1024) return PE_OK;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  if (allowed[dev].load(std::memory_order_acquire) >= smem) return PE_OK;
+  std::lock_guard<std::mutex> lock(g_dev_mutex);      // (the attribute is the last one set: it only grows)
+  if (allowed[dev].load(std::memory_order_relaxed) >= smem) return PE_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  allowed[dev].store(smem, std::memory_order_release);
+  return PE_OK;
+}
+
 // ---------------------------------------------------------------- forward
 struct ForwardPlan {
   int G, nv, threads;      // threads per row, vectors per thread, threads per block; G = 0: the kernel for rows of any width
@@ -52,7 +66,9 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
     const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 3072)));
     const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
     auto kernel = norm_forward_ring_kernel<T, E, RMS>;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+    static std::atomic<int> allowed[MAX_DEVICES];
+    const pe_status_t rc = allow_smem(kernel, allowed, smem);
+    if (rc != PE_OK) return rc;
     return launch_dependent(kernel, dim3((unsigned)blocks), threads, smem, st, x, gain, bias, rows, d, eps, y, mean, rstd, ring_G, wide, di->status_ptr);
   }
   const ForwardPlan p = plan_forward(d, E);
@@ -139,6 +155,13 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
 // Clusters of `size` blocks of this kernel that the device runs at a time (0: not known yet); more would wait for a second round.
 static std::atomic<int> g_clusters[MAX_DEVICES][NORM_MAX_CLUSTER + 1];
 
+template <typename T, int E, bool RMS, int KINDS, int MODE, bool SHORT>
+static pe_status_t launch_rows(const T* x, const T* dy, T* dx, const NormBackward& a, const BackwardPlan& p, int smem, cudaStream_t st) {
+  auto kernel = norm_backward_kernel<T, E, RMS, KINDS, MODE, SHORT>;
+  static std::atomic<int> allowed[MAX_DEVICES];
+  const pe_status_t rc = allow_smem(kernel, allowed, smem);
+  return rc != PE_OK ? rc : launch_dependent(kernel, dim3(p.blocks, p.slabs), p.G * p.groups, smem, st, x, dy, dx, a);
+}
 template <typename T, int E, bool RMS, int KINDS>
 static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, BackwardPlan& p, char* ws, cudaStream_t st) {
   const int threads = p.G * p.groups;
@@ -151,21 +174,13 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
   a.heads = reinterpret_cast<float*>(ws + p.heads_at);
   a.dev_status = di->status_ptr;
   a.row_means = reinterpret_cast<const float2*>(ws + p.means_at);
-  auto large_smem = [&](auto kernel) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess ? PE_OK : (cudaGetLastError(), PE_ERR_CUDA);
-  };
-  auto launch = [&](auto kernel) {
-    if (smem > 48 * 1024) {
-      const pe_status_t rc = large_smem(kernel);
-      if (rc != PE_OK) return rc;
-    }
-    return launch_dependent(kernel, dim3(p.blocks, p.slabs), threads, smem, st, x, dy, dx, a);
-  };
   if (p.mode == NORM_WHOLE)
-    return a.rows < 32ll * a.B || !p.kept ? launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_WHOLE, true>) : launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_WHOLE, false>);
+    return a.rows < 32ll * a.B || !p.kept ? launch_rows<T, E, RMS, KINDS, NORM_WHOLE, true>(x, dy, dx, a, p, smem, st)
+                                          : launch_rows<T, E, RMS, KINDS, NORM_WHOLE, false>(x, dy, dx, a, p, smem, st);
   if (p.mode == NORM_CLUSTER) {
     auto kernel = norm_backward_kernel<T, E, RMS, KINDS, NORM_CLUSTER, false>;
-    const pe_status_t rc = large_smem(kernel);
+    static std::atomic<int> allowed[MAX_DEVICES];
+    const pe_status_t rc = allow_smem(kernel, allowed, smem);
     if (rc != PE_OK) return rc;
     a.cluster = p.slabs;
     cudaLaunchConfig_t cfg = {};
@@ -194,7 +209,7 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
                                           a, reinterpret_cast<float2*>(ws + p.means_at));
   if (rc != PE_OK) return rc;
-  return launch(norm_backward_kernel<T, E, RMS, KINDS, NORM_SLAB, true>);
+  return launch_rows<T, E, RMS, KINDS, NORM_SLAB, true>(x, dy, dx, a, p, smem, st);
 }
 
 template <typename T>
