@@ -8,12 +8,46 @@
 namespace pe {
 
 constexpr int NS_MAX_STEPS = 100;
-constexpr int NS_MAX_PARTIALS = 64;
+constexpr int NS_MAX_PARTIALS = 512;
+constexpr int NS_PAIRS = 74;            // pairs of SMs that launches and the workspace are laid out for
+
+// How a product is cut: the tile's width, and slices of the contraction index where tiles are few.
+struct NsPlan {
+  int nt, splits;
+  long long units;      // tiles of a matrix
+};
+static long long ns_units(int rows, int cols, int nt, bool symmetric) {
+  const long long tiles_m = (rows + 255) / 256, tiles_n = (cols + nt - 1) / nt;
+  if (!symmetric) return tiles_m * tiles_n;
+  long long units = 0;
+  for (long long i = 0; i < tiles_m; ++i) units += tiles_n - i * (256 / nt);
+  return units;
+}
+// Times in microseconds: a stage of 64 (12 instructions of 256 x NT x 16), what a tile costs beside its stages (set-up, the first stage's way from
+// memory, write-out), and what joining slices costs.
+static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric) {
+  const int stages = (k + NS_BK - 1) / NS_BK;
+  NsPlan best = {128, 1, 0};
+  double best_us = 1e300;
+  for (int nt : {128, 256}) {
+    const long long units = ns_units(rows, cols, nt, symmetric), tiles = units * count;
+    const double stage_us = nt == 128 ? 0.50 : 0.92, fixed_us = nt == 128 ? 8.0 : 10.0;
+    for (int splits = 1; splits <= stages / 2 || splits == 1; ++splits) {
+      if (splits > 1 && tiles * splits > NS_PAIRS) break;
+      const long long waves = (tiles * splits + NS_PAIRS - 1) / NS_PAIRS;
+      const double us = waves * (((stages + splits - 1) / splits) * stage_us + fixed_us) + (splits > 1 ? 2.5 + 0.4 * splits : 0.0);
+      if (us < best_us) { best_us = us; best = {nt, splits, units}; }
+    }
+  }
+  return best;
+}
 
 struct NsLayout {
+  NsPlan gram, poly, apply;        // A = X X^T, A A, Q X
   int n, m, ld_m, ld_n, tall;
   int partials;                    // partial sums of a matrix's norm
-  size_t norms, x[2], a, q, total; // byte offsets into the workspace
+  int counters;                    // of split products, two words a tile
+  size_t norms, x[2], a, q, partial, counters_at, total; // byte offsets into the workspace
 };
 static bool ns_size_ok(int count, int rows, int cols) {
   return count >= 0 && rows >= 1 && cols >= 1 && rows <= (1 << 30) && cols <= (1 << 30) && (count == 0 || (long long)rows * cols <= ((1ll << 36) - 1) / count) && count <= 65535;
@@ -26,13 +60,24 @@ static NsLayout ns_layout(int count, int rows, int cols) {
   l.ld_m = (int)align_up(l.m, 8);      // TMA wants row pitches of 16 bytes
   l.ld_n = (int)align_up(l.n, 8);
   const long long elems = (long long)rows * cols;
-  l.partials = (int)std::min<long long>(NS_MAX_PARTIALS, (elems + 4095) / 4096);
+  l.partials = (int)std::min<long long>(NS_MAX_PARTIALS, (elems + 2047) / 2048);
   size_t at = 0;
   auto part = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
   l.norms = part((size_t)count * l.partials * sizeof(double));
   for (int k = 0; k < 2; ++k) l.x[k] = part(4ull * count * l.n * l.ld_m);      // two planes of halves
   l.a = part(4ull * count * l.n * l.ld_n);
   l.q = part(4ull * count * l.n * l.ld_n);
+  l.gram = plan_product(l.n, l.n, l.m, count, true);
+  l.poly = plan_product(l.n, l.n, l.n, count, true);
+  l.apply = plan_product(l.n, l.m, l.n, count, false);
+  size_t partial = 0;
+  for (const NsPlan* p : {&l.gram, &l.poly, &l.apply})
+    if (p->splits > 1) {
+      partial = std::max(partial, (size_t)(p->splits * p->units * count * 256 * p->nt) * sizeof(float));
+      l.counters = std::max(l.counters, (int)(2 * p->units * count));
+    }
+  l.partial = part(partial);
+  l.counters_at = part((size_t)l.counters * sizeof(unsigned int));
   l.total = at;
   return l;
 }
@@ -60,16 +105,15 @@ static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Ns
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NsTile<NT>::SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
     ready[dev >> 6].fetch_or(bit, std::memory_order_release);
   }
-  const long long tiles_m = (p.rows + 255) / 256;
   p.tiles_n = (p.cols + NT - 1) / NT;
-  long long units = 0;
-  if (EPI == NS_SYMMETRIC)
-    for (long long i = 0; i < tiles_m; ++i) units += p.tiles_n - i * (256 / NT);
-  else
-    units = tiles_m * p.tiles_n;
-  if (units * p.count >= (1ll << 30)) return PE_ERR_DIM;
-  p.units = (int)units;
-  return launch_dependent(kernel, dim3((unsigned)(2 * units * p.count)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, p);
+  return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, p);
+}
+template <bool B_MN, int EPI>
+static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, NsProduct p, cudaStream_t st) {
+  if (2 * plan.units * p.count >= (1ll << 31)) return PE_ERR_DIM;      // (then a single slice)
+  p.units = (int)plan.units;
+  p.splits = plan.splits;
+  return plan.nt == 256 ? launch_product<256, B_MN, EPI>(a, b, p, st) : launch_product<128, B_MN, EPI>(a, b, p, st);
 }
 
 // The iteration on what `s` describes; `out` holds the last product's output side.
@@ -78,33 +122,35 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   double* norms = reinterpret_cast<double*>(ws + l.norms);
   __half* x[2] = {reinterpret_cast<__half*>(ws + l.x[0]), reinterpret_cast<__half*>(ws + l.x[1])};
   __half *const a = reinterpret_cast<__half*>(ws + l.a), *const q = reinterpret_cast<__half*>(ws + l.q);
-  pe_status_t rc = launch_dependent(ns_norms_kernel, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms);
+  pe_status_t rc = launch_dependent(ns_norms_kernel, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms,
+                                    reinterpret_cast<unsigned int*>(ws + l.counters_at), l.counters);
   if (rc != PE_OK) return rc;
   const int tiles_m = (l.m + NS_INIT_TILE - 1) / NS_INIT_TILE, tiles_n = (l.n + NS_INIT_TILE - 1) / NS_INIT_TILE;
   rc = launch_dependent(ns_init_kernel, dim3((unsigned)(tiles_m * tiles_n), count), 256, 0, st, s, l.n, l.m, l.ld_m, l.tall, tiles_m, (const double*)norms,
                         l.partials, x[0], count);
   if (rc != PE_OK) return rc;
-  constexpr int NT = 128;
   CUtensorMap xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
   for (int k = 0; k < 2; ++k)
-    if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, NT / 2) != PE_OK ||
+    if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, l.gram.nt / 2) != PE_OK ||
         ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK) != PE_OK)
       return PE_ERR_CUDA;
-  if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, NT / 2) != PE_OK ||
+  if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, l.poly.nt / 2) != PE_OK ||
       ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK)
     return PE_ERR_CUDA;
   NsProduct p = out;
   p.count = count;
   p.dev_status = di->status_ptr;
   p.chunk = 2;
+  p.partial = reinterpret_cast<float*>(ws + l.partial);
+  p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
   for (int k = 0; k < steps; ++k) {
     const int from = k & 1;
     p.rows = p.cols = l.n; p.k = l.m; p.add = nullptr; p.out = a; p.ld = l.ld_n;
-    if ((rc = launch_product<NT, false, NS_SYMMETRIC>(xa[from], xb_rows[from], p, st)) != PE_OK) return rc;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], p, st)) != PE_OK) return rc;
     p.k = l.n; p.add = a; p.out = q;
-    if ((rc = launch_product<NT, false, NS_SYMMETRIC>(aa, ab, p, st)) != PE_OK) return rc;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, p, st)) != PE_OK) return rc;
     p.cols = l.m; p.add = nullptr; p.out = x[from ^ 1]; p.ld = l.ld_m;
-    rc = k + 1 < steps ? launch_product<NT, true, NS_PLANES>(qa, xb_cols[from], p, st) : launch_product<NT, true, NS_FINAL>(qa, xb_cols[from], p, st);
+    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], p, st);
     if (rc != PE_OK) return rc;
   }
   return PE_OK;

@@ -49,19 +49,35 @@ __device__ __forceinline__ float ns_source_value(const NsSource& s, long long i)
   return s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * (s.sum_g[i] * s.grad_scale)) : m;
 }
 // Squared Frobenius norms, as gridDim.x partial sums per matrix (gridDim.y matrices), in 64 bits: no scale of the gradients overflows or vanishes.
-// Updates the momentum by the way.
+// Updates the momentum by the way, and zeroes the counters of split products.
 constexpr int NS_NORM_THREADS = 256;
 __global__ void __launch_bounds__(NS_NORM_THREADS)
-ns_norms_kernel(NsSource s, long long elems, double* __restrict__ partial) {
+ns_norms_kernel(NsSource s, long long elems, double* __restrict__ partial, unsigned int* __restrict__ counters, int n_counters) {
   sm100::griddep_launch_dependents();
   sm100::griddep_wait();
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int k = threadIdx.x; k < n_counters; k += blockDim.x) counters[k] = 0u;
   __shared__ double warp_sum[NS_NORM_THREADS / 32];
   const long long base = (long long)blockIdx.y * elems, stride = (long long)gridDim.x * blockDim.x;
   double sum = 0.0;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < elems; i += stride) {
-    if (!s.given) s.m[base + i] = fmaf(s.beta, s.m[base + i], (1.f - s.beta) * (s.sum_g[base + i] * s.grad_scale));
-    const double v = ns_source_value(s, base + i);
-    sum += v * v;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < elems; i += 4 * stride) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const long long at = base + i + k * stride;
+      v[k] = 0.f;
+      if (i + k * stride < elems) {
+        if (s.given) {
+          v[k] = ns_source_value(s, at);
+        } else {
+          const float g = s.sum_g[at] * s.grad_scale, m = fmaf(s.beta, s.m[at], (1.f - s.beta) * g);
+          s.m[at] = m;
+          v[k] = s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * g) : m;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum += (double)v[k] * (double)v[k];
   }
 #pragma unroll
   for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
@@ -137,6 +153,9 @@ struct NsProduct {
   int tiles_n;                   // column tiles; NS_SYMMETRIC: those that touch the upper triangle are worked on
   int units;                     // tiles per matrix
   int count, chunk;
+  int splits;                    // slices of the contraction index, each a pair's; the last one done adds the partial tiles up in their order
+  float* partial;                // [splits][units * count][2][8 warps][NT / 2][32], where there are several
+  unsigned int* counters;        // [units * count][2], zero before and after a product
   const __half* add;             // NS_SYMMETRIC: NULL, or planes [2][count][rows][ld] of A: the result is a I + b A + c (product)
   __half* out;                   // planes [2][count][rows][ld]
   int ld;
@@ -167,35 +186,23 @@ __host__ __device__ constexpr uint32_t ns_idesc(int N, bool b_mn) {
   return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
 }
 
-// One thread's row `r`, columns c .. c + 31 of the tile: scaled values to both planes, and to their mirror image.
-__device__ __forceinline__ void ns_store_planes(const NsProduct& p, size_t mat_row0, int r, int c, const float (&v)[32], bool symmetric) {
-  const size_t plane = (size_t)p.count * p.rows * p.ld;
+// One thread's row of 32 scaled values to both planes, at element `at` (a multiple of 8); columns from `left` on are outside (and within the row's padding up to a
+// multiple of 8).
+__device__ __forceinline__ void ns_store_row(__half* at, size_t plane, int left, const float (&v)[32]) {
 #pragma unroll
   for (int j = 0; j < 32; j += 8) {
-    if (c + j >= p.cols) continue;
-    __half hi[8], lo[8];
+    if (j >= left) break;
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ns_split(v[j + e], hi[e], lo[e]);
-    if (r < p.rows) {
-      __half* at = p.out + (mat_row0 + r) * p.ld + c + j;
-      if (!symmetric || c + j >= r) {
-        *reinterpret_cast<uint4*>(at) = make_uint4(ns_pack(hi[0], hi[1]), ns_pack(hi[2], hi[3]), ns_pack(hi[4], hi[5]), ns_pack(hi[6], hi[7]));
-        *reinterpret_cast<uint4*>(at + plane) = make_uint4(ns_pack(lo[0], lo[1]), ns_pack(lo[2], lo[3]), ns_pack(lo[4], lo[5]), ns_pack(lo[6], lo[7]));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + j + e >= r) { at[e] = hi[e]; at[plane + e] = lo[e]; }
-      }
-      if (symmetric) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + j + e > r && c + j + e < p.rows) {
-            __half* mirror = p.out + (mat_row0 + c + j + e) * p.ld + r;
-            mirror[0] = hi[e];
-            mirror[plane] = lo[e];
-          }
-      }
+    for (int e = 0; e < 4; ++e) {
+      __half h0, l0, h1, l1;
+      ns_split(v[j + 2 * e], h0, l0);
+      ns_split(v[j + 2 * e + 1], h1, l1);
+      hi[e] = ns_pack(h0, h1);
+      lo[e] = ns_pack(l0, l1);
     }
+    *reinterpret_cast<uint4*>(at + j) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(at + plane + j) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
@@ -217,10 +224,12 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   static_assert(8 * (2 * STAGES + 2 * ACC) + 16 <= Tile::BAR_BYTES, "barrier area too small");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+  volatile int* split_flag = reinterpret_cast<volatile int*>(tail + 12);
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const long long unit = blockIdx.x >> 1;
+  const int slice = (int)(blockIdx.x >> 1) % p.splits;
+  const long long unit = (blockIdx.x >> 1) / p.splits;
   const int mat = (int)(unit / p.units);
   int tile_m = 0, tile_n = (int)(unit - (long long)mat * p.units);
   if constexpr (EPI == NS_SYMMETRIC) {      // row by row, the tiles from the diagonal on
@@ -231,7 +240,8 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     tile_m = tile_n / p.tiles_n;
     tile_n -= tile_m * p.tiles_n;
   }
-  const int stages = (p.k + NS_BK - 1) / NS_BK, n_acc = (stages + p.chunk - 1) / p.chunk;
+  const int all_stages = (p.k + NS_BK - 1) / NS_BK, stage0 = (int)((long long)all_stages * slice / p.splits);
+  const int stages = (int)((long long)all_stages * (slice + 1) / p.splits) - stage0, n_acc = (stages + p.chunk - 1) / p.chunk;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -257,7 +267,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       if (elect_one()) {
         if (rank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * Tile::STAGE_BYTES);
         const uint32_t leader_full = map_to_cta(full_bar(s), 0), dst = smem_base + s * Tile::STAGE_BYTES;
-        const int k0 = ks * NS_BK, row = tile_m * 256 + (int)rank * 128, col = tile_n * NT + (int)rank * (NT / 2);
+        const int k0 = (stage0 + ks) * NS_BK, row = tile_m * 256 + (int)rank * 128, col = tile_n * NT + (int)rank * (NT / 2);
 #pragma unroll
         for (int plane = 0; plane < 2; ++plane) {
           const int z = plane * p.count + mat;
@@ -294,7 +304,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           const uint32_t d_tmem = tmem_base + (uint32_t)(buf * NT);
           const uint32_t a_src = smem_base + s * Tile::STAGE_BYTES, b_src = a_src + 2 * Tile::A_PLANE;
           uint32_t accumulate = in_chunk > 0;
-          const int k_left = p.k - ks * NS_BK;
+          const int k_left = p.k - (stage0 + ks) * NS_BK;
 #pragma unroll
           for (int term = 0; term < 3; ++term) {        // hi lo, lo hi, hi hi
             const uint32_t ap = a_src + (term == 1 ? Tile::A_PLANE : 0), bp = b_src + (term == 0 ? Tile::B_PLANE : 0);
@@ -341,51 +351,106 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int j = 0; j < 32; ++j) acc[c * 32 + j] += __uint_as_float(v[j]);
       }
     }
-    if (ok && EPI == NS_FINAL) ok = *reinterpret_cast<volatile unsigned int*>(p.dev_status) == 0u;      // an earlier product may have given up
-    if (ok) {
+    bool write = true;
+    if (p.splits > 1) {      // (all eight warps of the block, whatever their waits said)
+      const size_t tiles = (size_t)p.units * p.count, mine = ((size_t)unit * 2 + rank) * 8 + (warp - 2);
+      float* at = p.partial + (slice * tiles * 16 + mine) * (COLS * 32) + lane;
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) __stcg(at + j * 32, acc[j]);
+      __threadfence();
+      named_bar_sync(1, 256);
+      if (threadIdx.x == 64) {
+        const unsigned int before = atomicAdd(p.counters + unit * 2 + rank, 1u);
+        if (before == (unsigned int)p.splits - 1) p.counters[unit * 2 + rank] = 0u;
+        *split_flag = before == (unsigned int)p.splits - 1;
+      }
+      named_bar_sync(1, 256);
+      write = *split_flag != 0;
+      if (write) {
+        __threadfence();
+        at = p.partial + mine * (COLS * 32) + lane;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[j] = __ldcg(at + j * 32);
+        for (int k = 1; k < p.splits; ++k) {
+          at += tiles * 16 * (COLS * 32);
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) acc[j] += __ldcg(at + j * 32);
+        }
+      }
+    }
+    if (EPI == NS_FINAL && *reinterpret_cast<volatile unsigned int*>(p.dev_status) != 0u) write = false;      // an earlier product may have given up
+    if (ok && write) {
+      // A warp's 32 x 32 pieces.  Lanes hold rows; an exchange of lanes and registers turns a piece over, for its mirror image and for results whose
+      // rows are to be written along the lanes.
+      const int row0 = tile_m * 256 + (int)rank * 128 + q * 32;
 #pragma unroll
       for (int c = 0; c < COLS / 32; ++c) {
         const int col = c0 + c * 32;
-        if (col < p.cols) {      // (the warp as one)
-          float v[32];
-          if constexpr (EPI == NS_FINAL) {
+        if (col >= p.cols || row0 >= p.rows) continue;      // (the warp as one)
+        float v[32];
+        if constexpr (EPI == NS_FINAL) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * (NS_UNSCALE * NS_UNSCALE);
-            if (r < p.rows) {
-              const size_t base = (size_t)mat * p.rows * p.cols;
+          for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * (NS_UNSCALE * NS_UNSCALE);
+          if (!p.transposed) warp_transpose(v, lane);
+          // v[j]: row row0 + j, column col + lane, or (transposed) the other way round: along the lanes in memory either way
+          const int slow0 = p.transposed ? col : row0, fast = (p.transposed ? row0 : col) + lane;
+          const int n_slow = p.transposed ? p.cols : p.rows, n_fast = p.transposed ? p.rows : p.cols;
+          const size_t base = (size_t)mat * p.rows * p.cols + (size_t)slow0 * n_fast + fast;
+          if (fast < n_fast) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
+            for (int j = 0; j < 32; ++j) {
+              if (slow0 + j < n_slow) {
+                const size_t at = base + (size_t)j * n_fast;
+                if (p.result) {
+                  if (p.out_bf16) static_cast<__nv_bfloat16*>(p.result)[at] = __float2bfloat16_rn(v[j]);
+                  else static_cast<float*>(p.result)[at] = v[j];
+                } else {
+                  const float th = p.theta[at], next = th - p.step * v[j] - p.wd * th;
+                  p.theta[at] = next;
+                  if (p.theta_lp) p.theta_lp[at] = __float2bfloat16_rn(next);
+                }
+              }
+            }
+          }
+        } else {
+          const size_t mat0 = (size_t)mat * p.rows, plane = (size_t)p.count * p.rows * p.ld;
+          if (EPI == NS_SYMMETRIC && col + 31 < row0) continue;      // below the diagonal: the mirror image of another piece
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * NS_UNSCALE;      // 2^12 of the value
+          if constexpr (EPI == NS_SYMMETRIC) {
+            if (p.add && r < p.rows) {
+              const __half* at = p.add + (mat0 + r) * p.ld + col;
+#pragma unroll
+              for (int j = 0; j < 32; j += 8) {
                 if (col + j < p.cols) {
-                  const size_t at = base + (p.transposed ? (size_t)(col + j) * p.rows + r : (size_t)r * p.cols + col + j);
-                  if (p.result) {
-                    if (p.out_bf16) static_cast<__nv_bfloat16*>(p.result)[at] = __float2bfloat16_rn(v[j]);
-                    else static_cast<float*>(p.result)[at] = v[j];
-                  } else {
-                    const float th = p.theta[at], next = th - p.step * v[j] - p.wd * th;
-                    p.theta[at] = next;
-                    if (p.theta_lp) p.theta_lp[at] = __float2bfloat16_rn(next);
+                  const uint4 h4 = *reinterpret_cast<const uint4*>(at + j), l4 = *reinterpret_cast<const uint4*>(at + plane + j);
+                  const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hw[e])), l = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
+                    v[j + 2 * e] = fmaf(NS_C, v[j + 2 * e], NS_B * (h.x + l.x));
+                    v[j + 2 * e + 1] = fmaf(NS_C, v[j + 2 * e + 1], NS_B * (h.y + l.y));
                   }
                 }
               }
             }
-          } else {
+            if (p.add && col == row0) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * NS_UNSCALE;      // 2^12 of the value
-            const size_t row0 = (size_t)mat * p.rows;
-            if constexpr (EPI == NS_SYMMETRIC) {
-              if (p.add && r < p.rows) {
-                const size_t plane = (size_t)p.count * p.rows * p.ld;
-                const __half* at = p.add + (row0 + r) * p.ld + col;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                  const bool in = col + j < p.cols;
-                  const float A = in ? __half2float(at[j]) + __half2float(at[plane + j]) : 0.f;
-                  v[j] = fmaf(NS_C, v[j], fmaf(NS_B, A, r == col + j ? NS_A * NS_SCALE : 0.f));
-                }
-              }
+              for (int j = 0; j < 32; ++j)
+                if (j == lane) v[j] += NS_A * NS_SCALE;
             }
-            ns_store_planes(p, row0, r, col, v, EPI == NS_SYMMETRIC);
+            float turned[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) turned[j] = v[j];
+            warp_transpose(turned, lane);
+            if (col == row0) {      // on the diagonal: what is above it on both sides
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = j >= lane ? v[j] : turned[j];
+            } else if (col + lane < p.cols) {
+              ns_store_row(p.out + (mat0 + col + lane) * p.ld + row0, plane, p.rows - row0, turned);
+            }
           }
+          if (r < p.rows) ns_store_row(p.out + (mat0 + r) * p.ld + col, plane, p.cols - col, v);
         }
       }
     }
