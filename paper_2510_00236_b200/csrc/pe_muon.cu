@@ -82,20 +82,21 @@ static NsLayout ns_layout(int count, int rows, int cols) {
   return l;
 }
 
-// Planes [2 * count][rows][ld] of halves, `cols` columns of them data; one box = 64 columns (128 bytes, swizzled) x box_rows rows.
-static pe_status_t ns_map(CUtensorMap* map, const void* base, int planes, int rows, int cols, int ld, int box_rows) {
+// Planes [2 * count][rows][ld] of halves, `cols` columns of them data; one box = 64 columns (128 bytes, swizzled) x box_rows rows, or
+// a piece of 32 columns (64 bytes).
+static pe_status_t ns_map(CUtensorMap* map, const void* base, int planes, int rows, int cols, int ld, int box_rows, bool piece = false) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return PE_ERR_CUDA;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
-  cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, estr[3] = {1u, 1u, 1u};
+  cuuint32_t box[3] = {piece ? 32u : 64u, (cuuint32_t)box_rows, 1u}, estr[3] = {1u, 1u, 1u};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             piece ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? PE_OK : PE_ERR_CUDA;
 }
 
 template <int NT, bool B_MN, int EPI>
-static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, NsProduct p, cudaStream_t st) {
+static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, NsProduct p, cudaStream_t st) {
   static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];      // devices whose kernel attribute is set
   auto kernel = ns_product_kernel<NT, B_MN, EPI>;
   int dev = 0;
@@ -106,14 +107,14 @@ static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Ns
     ready[dev >> 6].fetch_or(bit, std::memory_order_release);
   }
   p.tiles_n = (p.cols + NT - 1) / NT;
-  return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, p);
+  return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, out, p);
 }
 template <bool B_MN, int EPI>
-static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, NsProduct p, cudaStream_t st) {
+static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, NsProduct p, cudaStream_t st) {
   if (2 * plan.units * p.count >= (1ll << 31)) return PE_ERR_DIM;      // (then a single slice)
   p.units = (int)plan.units;
   p.splits = plan.splits;
-  return plan.nt == 256 ? launch_product<256, B_MN, EPI>(a, b, p, st) : launch_product<128, B_MN, EPI>(a, b, p, st);
+  return plan.nt == 256 ? launch_product<256, B_MN, EPI>(a, b, out, p, st) : launch_product<128, B_MN, EPI>(a, b, out, p, st);
 }
 
 // The iteration on what `s` describes; `out` holds the last product's output side.
@@ -129,13 +130,14 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   rc = launch_dependent(ns_init_kernel, dim3((unsigned)(tiles_m * tiles_n), count), 256, 0, st, s, l.n, l.m, l.ld_m, l.tall, tiles_m, (const double*)norms,
                         l.partials, x[0], count);
   if (rc != PE_OK) return rc;
-  CUtensorMap xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
+  CUtensorMap xo[2], ao, qo, xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
   for (int k = 0; k < 2; ++k)
     if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, l.gram.nt / 2) != PE_OK ||
-        ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK) != PE_OK)
+        ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK) != PE_OK || ns_map(&xo[k], x[k], 2 * count, l.n, l.m, l.ld_m, 32, true) != PE_OK)
       return PE_ERR_CUDA;
   if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, l.poly.nt / 2) != PE_OK ||
-      ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK)
+      ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ao, a, 2 * count, l.n, l.n, l.ld_n, 32, true) != PE_OK ||
+      ns_map(&qo, q, 2 * count, l.n, l.n, l.ld_n, 32, true) != PE_OK)
     return PE_ERR_CUDA;
   NsProduct p = out;
   p.count = count;
@@ -145,12 +147,12 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
   for (int k = 0; k < steps; ++k) {
     const int from = k & 1;
-    p.rows = p.cols = l.n; p.k = l.m; p.add = nullptr; p.out = a; p.ld = l.ld_n;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], p, st)) != PE_OK) return rc;
-    p.k = l.n; p.add = a; p.out = q;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, p, st)) != PE_OK) return rc;
-    p.cols = l.m; p.add = nullptr; p.out = x[from ^ 1]; p.ld = l.ld_m;
-    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], p, st);
+    p.rows = p.cols = l.n; p.k = l.m; p.add = nullptr; p.ld = l.ld_n;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], ao, p, st)) != PE_OK) return rc;
+    p.k = l.n; p.add = a;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, qo, p, st)) != PE_OK) return rc;
+    p.cols = l.m; p.add = nullptr;
+    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], xo[from ^ 1], p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], xo[from ^ 1], p, st);
     if (rc != PE_OK) return rc;
   }
   return PE_OK;

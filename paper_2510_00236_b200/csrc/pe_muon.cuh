@@ -157,8 +157,7 @@ struct NsProduct {
   float* partial;                // [splits][units * count][2][8 warps][NT / 2][32], where there are several
   unsigned int* counters;        // [units * count][2], zero before and after a product
   const __half* add;             // NS_SYMMETRIC: NULL, or planes [2][count][rows][ld] of A: the result is a I + b A + c (product)
-  __half* out;                   // planes [2][count][rows][ld]
-  int ld;
+  int ld;                        // of `add`
   // NS_FINAL: the result itself, [rows, cols] per matrix, or transposed: [cols, rows]
   int transposed, out_bf16;
   void* result;                  // as given, or NULL and
@@ -186,12 +185,17 @@ __host__ __device__ constexpr uint32_t ns_idesc(int N, bool b_mn) {
   return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
 }
 
-// One thread's row of 32 scaled values to both planes, at element `at` (a multiple of 8); columns from `left` on are outside (and within the row's padding up to a
-// multiple of 8).
-__device__ __forceinline__ void ns_store_row(__half* at, size_t plane, int left, const float (&v)[32]) {
+// Write-out of planes.  A warp stages 32 x 32 pieces in the operand buffers (which nothing reads any more) as 32 rows of 64 bytes with the 64-byte swizzle,
+// and TMA stores them; what lies outside the matrix is dropped there.  (Stored from registers, a row of 64 bytes to a lane touches 32 lines per instruction:
+// 6 us for a 256 x 128 tile and its mirror image.)
+constexpr int NS_PIECE = 32 * 64;
+__device__ __forceinline__ uint32_t ns_piece_offset(int row, int col) {      // bytes; col: of halves
+  return (uint32_t)(row * 64 + (((col >> 3) ^ (row >> 1)) & 3) * 16 + (col & 7) * 2);
+}
+// a lane's row
+__device__ __forceinline__ void ns_stage_row(uint8_t* piece, int lane, const float (&v)[32]) {      // hi, then lo NS_PIECE bytes on
 #pragma unroll
   for (int j = 0; j < 32; j += 8) {
-    if (j >= left) break;
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -201,14 +205,35 @@ __device__ __forceinline__ void ns_store_row(__half* at, size_t plane, int left,
       hi[e] = ns_pack(h0, h1);
       lo[e] = ns_pack(l0, l1);
     }
-    *reinterpret_cast<uint4*>(at + j) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(at + plane + j) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    *reinterpret_cast<uint4*>(piece + ns_piece_offset(lane, j)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(piece + NS_PIECE + ns_piece_offset(lane, j)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
+}
+// the same row as a column; of a piece on the diagonal: each value from the diagonal on, to both places
+__device__ __forceinline__ void ns_stage_column(uint8_t* piece, int lane, const float (&v)[32], bool diagonal) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    __half h, l;
+    ns_split(v[j], h, l);
+    if (!diagonal || j >= lane) {
+      *reinterpret_cast<__half*>(piece + ns_piece_offset(j, lane)) = h;
+      *reinterpret_cast<__half*>(piece + NS_PIECE + ns_piece_offset(j, lane)) = l;
+      if (diagonal) {
+        *reinterpret_cast<__half*>(piece + ns_piece_offset(lane, j)) = h;
+        *reinterpret_cast<__half*>(piece + NS_PIECE + ns_piece_offset(lane, j)) = l;
+      }
+    }
+  }
+}
+__device__ __forceinline__ void ns_store_piece(const CUtensorMap* map, uint32_t src, int col, int row, int plane) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(col),
+               "r"(row), "r"(plane) : "memory");
 }
 
 template <int NT, bool B_MN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NS_THREADS, 1)
-ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ NsProduct p) {
+ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                  const __grid_constant__ NsProduct p) {
   using namespace sm100;
   using Tile = NsTile<NT>;
   constexpr int STAGES = Tile::STAGES, ACC = 2, COLS = NT / 2;
@@ -380,36 +405,59 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     if (EPI == NS_FINAL && *reinterpret_cast<volatile unsigned int*>(p.dev_status) != 0u) write = false;      // an earlier product may have given up
     if (ok && write) {
-      // A warp's 32 x 32 pieces.  Lanes hold rows; an exchange of lanes and registers turns a piece over, for its mirror image and for results whose
-      // rows are to be written along the lanes.
+      // A warp's 32 x 32 pieces; lanes hold rows.
       const int row0 = tile_m * 256 + (int)rank * 128 + q * 32;
+      uint8_t* const staging = smem_gen + (warp - 2) * (8 * NS_PIECE);
+      const uint32_t staging_s = smem_base + (uint32_t)(warp - 2) * (8 * NS_PIECE);
+      static_assert(8 * 8 * NS_PIECE <= STAGES * Tile::STAGE_BYTES, "two pieces, their mirror images and two planes for each of eight warps");
+      int used = 0;      // pieces staged
 #pragma unroll
       for (int c = 0; c < COLS / 32; ++c) {
         const int col = c0 + c * 32;
         if (col >= p.cols || row0 >= p.rows) continue;      // (the warp as one)
         float v[32];
         if constexpr (EPI == NS_FINAL) {
+          // along the lanes in memory: rows of the result by way of shared memory, columns (a transposed result) as they are
+          float* turn = reinterpret_cast<float*>(staging);      // [32][33]
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * (NS_UNSCALE * NS_UNSCALE);
-          if (!p.transposed) warp_transpose(v, lane);
-          // v[j]: row row0 + j, column col + lane, or (transposed) the other way round: along the lanes in memory either way
+          if (!p.transposed) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = turn[j * 33 + lane];
+          }
           const int slow0 = p.transposed ? col : row0, fast = (p.transposed ? row0 : col) + lane;
-          const int n_slow = p.transposed ? p.cols : p.rows, n_fast = p.transposed ? p.rows : p.cols;
+          const int n_slow = (p.transposed ? p.cols : p.rows) - slow0, n_fast = p.transposed ? p.rows : p.cols;
           const size_t base = (size_t)mat * p.rows * p.cols + (size_t)slow0 * n_fast + fast;
           if (fast < n_fast) {
+            if (!p.result) {
+              float* th = p.theta + base;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (slow0 + j < n_slow) {
-                const size_t at = base + (size_t)j * n_fast;
-                if (p.result) {
-                  if (p.out_bf16) static_cast<__nv_bfloat16*>(p.result)[at] = __float2bfloat16_rn(v[j]);
-                  else static_cast<float*>(p.result)[at] = v[j];
-                } else {
-                  const float th = p.theta[at], next = th - p.step * v[j] - p.wd * th;
-                  p.theta[at] = next;
-                  if (p.theta_lp) p.theta_lp[at] = __float2bfloat16_rn(next);
-                }
+              for (int j0 = 0; j0 < 32; j0 += 8) {      // eight loads in flight
+                float old[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) old[j] = j0 + j < n_slow ? th[(size_t)(j0 + j) * n_fast] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (j0 + j < n_slow) {
+                    const float next = old[j] - p.step * v[j0 + j] - p.wd * old[j];
+                    th[(size_t)(j0 + j) * n_fast] = next;
+                    if (p.theta_lp) p.theta_lp[base + (size_t)(j0 + j) * n_fast] = __float2bfloat16_rn(next);
+                  }
               }
+            } else if (p.out_bf16) {
+              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.result) + base;
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (j < n_slow) to[(size_t)j * n_fast] = __float2bfloat16_rn(v[j]);
+            } else {
+              float* to = static_cast<float*>(p.result) + base;
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (j < n_slow) to[(size_t)j * n_fast] = v[j];
             }
           }
         } else {
@@ -417,42 +465,59 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           if (EPI == NS_SYMMETRIC && col + 31 < row0) continue;      // below the diagonal: the mirror image of another piece
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * NS_UNSCALE;      // 2^12 of the value
+          const bool diagonal = EPI == NS_SYMMETRIC && col == row0;
           if constexpr (EPI == NS_SYMMETRIC) {
-            if (p.add && r < p.rows) {
-              const __half* at = p.add + (mat0 + r) * p.ld + col;
+            if (p.add) {
+              if (r < p.rows) {
+                const __half* at = p.add + (mat0 + r) * p.ld + col;
 #pragma unroll
-              for (int j = 0; j < 32; j += 8) {
-                if (col + j < p.cols) {
-                  const uint4 h4 = *reinterpret_cast<const uint4*>(at + j), l4 = *reinterpret_cast<const uint4*>(at + plane + j);
-                  const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+                for (int j = 0; j < 32; j += 8) {
+                  if (col + j < p.cols) {
+                    const uint4 h4 = *reinterpret_cast<const uint4*>(at + j), l4 = *reinterpret_cast<const uint4*>(at + plane + j);
+                    const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hw[e])), l = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
-                    v[j + 2 * e] = fmaf(NS_C, v[j + 2 * e], NS_B * (h.x + l.x));
-                    v[j + 2 * e + 1] = fmaf(NS_C, v[j + 2 * e + 1], NS_B * (h.y + l.y));
+                    for (int e = 0; e < 4; ++e) {
+                      const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hw[e])), l = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
+                      v[j + 2 * e] = fmaf(NS_C, v[j + 2 * e], NS_B * (h.x + l.x));
+                      v[j + 2 * e + 1] = fmaf(NS_C, v[j + 2 * e + 1], NS_B * (h.y + l.y));
+                    }
                   }
                 }
               }
-            }
-            if (p.add && col == row0) {
+              if (diagonal) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (j == lane) v[j] += NS_A * NS_SCALE;
-            }
-            float turned[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) turned[j] = v[j];
-            warp_transpose(turned, lane);
-            if (col == row0) {      // on the diagonal: what is above it on both sides
-#pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] = j >= lane ? v[j] : turned[j];
-            } else if (col + lane < p.cols) {
-              ns_store_row(p.out + (mat0 + col + lane) * p.ld + row0, plane, p.rows - row0, turned);
+                for (int j = 0; j < 32; ++j)
+                  if (j == lane) v[j] += NS_A * NS_SCALE;
+              }
             }
           }
-          if (r < p.rows) ns_store_row(p.out + (mat0 + r) * p.ld + col, plane, p.cols - col, v);
+          uint8_t* piece = staging + (used & 1) * (4 * NS_PIECE);
+          const uint32_t piece_s = staging_s + (uint32_t)(used & 1) * (4 * NS_PIECE);
+          if (used >= 2) {      // the stores of the piece before last have read this place
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+          }
+          if (diagonal) {
+            ns_stage_column(piece, lane, v, true);
+          } else {
+            ns_stage_row(piece, lane, v);
+            if (EPI == NS_SYMMETRIC) ns_stage_column(piece + 2 * NS_PIECE, lane, v, false);
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            ns_store_piece(&map_out, piece_s, col, row0, mat);
+            ns_store_piece(&map_out, piece_s + NS_PIECE, col, row0, p.count + mat);
+            if (EPI == NS_SYMMETRIC && !diagonal) {
+              ns_store_piece(&map_out, piece_s + 2 * NS_PIECE, row0, col, mat);
+              ns_store_piece(&map_out, piece_s + 3 * NS_PIECE, row0, col, p.count + mat);
+            }
+            bulk_commit_group();
+          }
+          ++used;
         }
       }
+      if (EPI != NS_FINAL && lane == 0) bulk_wait_all();
     }
   }
 
