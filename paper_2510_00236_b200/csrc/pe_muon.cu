@@ -29,9 +29,9 @@ static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric)
   const int stages = (k + NS_BK - 1) / NS_BK;
   NsPlan best = {128, 1, 0};
   double best_us = 1e300;
-  for (int nt : {128, 256}) {
+  for (int nt : {64, 128, 256}) {
     const long long units = ns_units(rows, cols, nt, symmetric), tiles = units * count;
-    const double stage_us = nt == 128 ? 0.50 : 0.92, fixed_us = nt == 128 ? 8.0 : 10.0;
+    const double stage_us = nt == 64 ? 0.30 : nt == 128 ? 0.50 : 0.92, fixed_us = nt == 64 ? 5.0 : nt == 128 ? 6.5 : 9.0;
     for (int splits = 1; splits <= stages / 2 || splits == 1; ++splits) {
       if (splits > 1 && tiles * splits > NS_PAIRS) break;
       const long long waves = (tiles * splits + NS_PAIRS - 1) / NS_PAIRS;
@@ -96,7 +96,7 @@ static pe_status_t ns_map(CUtensorMap* map, const void* base, int planes, int ro
 }
 
 template <int NT, bool B_MN, int EPI>
-static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, NsProduct p, cudaStream_t st) {
+static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const CUtensorMap& add, NsProduct p, cudaStream_t st) {
   static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];      // devices whose kernel attribute is set
   auto kernel = ns_product_kernel<NT, B_MN, EPI>;
   int dev = 0;
@@ -107,14 +107,15 @@ static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, co
     ready[dev >> 6].fetch_or(bit, std::memory_order_release);
   }
   p.tiles_n = (p.cols + NT - 1) / NT;
-  return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, out, p);
+  return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, out, add, p);
 }
 template <bool B_MN, int EPI>
-static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, NsProduct p, cudaStream_t st) {
+static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const CUtensorMap& add, NsProduct p, cudaStream_t st) {
   if (2 * plan.units * p.count >= (1ll << 31)) return PE_ERR_DIM;      // (then a single slice)
   p.units = (int)plan.units;
   p.splits = plan.splits;
-  return plan.nt == 256 ? launch_product<256, B_MN, EPI>(a, b, out, p, st) : launch_product<128, B_MN, EPI>(a, b, out, p, st);
+  if (plan.nt == 64) return launch_product<64, B_MN, EPI>(a, b, out, add, p, st);
+  return plan.nt == 256 ? launch_product<256, B_MN, EPI>(a, b, out, add, p, st) : launch_product<128, B_MN, EPI>(a, b, out, add, p, st);
 }
 
 // The iteration on what `s` describes; `out` holds the last product's output side.
@@ -133,7 +134,7 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   CUtensorMap xo[2], ao, qo, xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
   for (int k = 0; k < 2; ++k)
     if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, l.gram.nt / 2) != PE_OK ||
-        ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK) != PE_OK || ns_map(&xo[k], x[k], 2 * count, l.n, l.m, l.ld_m, 32, true) != PE_OK)
+        ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK, l.apply.nt == 64) != PE_OK || ns_map(&xo[k], x[k], 2 * count, l.n, l.m, l.ld_m, 32, true) != PE_OK)
       return PE_ERR_CUDA;
   if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, l.poly.nt / 2) != PE_OK ||
       ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ao, a, 2 * count, l.n, l.n, l.ld_n, 32, true) != PE_OK ||
@@ -147,12 +148,12 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
   for (int k = 0; k < steps; ++k) {
     const int from = k & 1;
-    p.rows = p.cols = l.n; p.k = l.m; p.add = nullptr; p.ld = l.ld_n;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], ao, p, st)) != PE_OK) return rc;
-    p.k = l.n; p.add = a;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, qo, p, st)) != PE_OK) return rc;
-    p.cols = l.m; p.add = nullptr;
-    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], xo[from ^ 1], p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], xo[from ^ 1], p, st);
+    p.rows = p.cols = l.n; p.k = l.m; p.add = 0;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], ao, ao, p, st)) != PE_OK) return rc;
+    p.k = l.n; p.add = 1;
+    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, qo, ao, p, st)) != PE_OK) return rc;
+    p.cols = l.m; p.add = 0;
+    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], xo[from ^ 1], ao, p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], xo[from ^ 1], ao, p, st);
     if (rc != PE_OK) return rc;
   }
   return PE_OK;

@@ -156,8 +156,7 @@ struct NsProduct {
   int splits;                    // slices of the contraction index, each a pair's; the last one done adds the partial tiles up in their order
   float* partial;                // [splits][units * count][2][8 warps][NT / 2][32], where there are several
   unsigned int* counters;        // [units * count][2], zero before and after a product
-  const __half* add;             // NS_SYMMETRIC: NULL, or planes [2][count][rows][ld] of A: the result is a I + b A + c (product)
-  int ld;                        // of `add`
+  int add;                       // NS_SYMMETRIC: 0, or 1: the result is a I + b A + c (product), A by map_add
   // NS_FINAL: the result itself, [rows, cols] per matrix, or transposed: [cols, rows]
   int transposed, out_bf16;
   void* result;                  // as given, or NULL and
@@ -169,22 +168,6 @@ struct NsProduct {
 constexpr int NS_THREADS = 320;
 constexpr int NS_BK = 64;
 constexpr int NS_TMEM_COLS = 512;
-template <int NT>
-struct NsTile {
-  static constexpr int A_PLANE = 128 * 128;                  // 128 rows of 64 halves
-  static constexpr int B_PLANE = (NT / 2) * 128;
-  static constexpr int STAGE_BYTES = 2 * A_PLANE + 2 * B_PLANE;
-  static constexpr int STAGES = NT == 256 ? 3 : 4;
-  static constexpr int BAR_BYTES = 256;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + BAR_BYTES + 1024;
-};
-enum : int { NS_WAIT_EMPTY = 101, NS_WAIT_FULL = 102, NS_WAIT_ACC_EMPTY = 103, NS_WAIT_ACC_FULL = 104 };
-
-// Instruction descriptor: IEEE half operands, A row by row (K-major), B row by row or (b_mn) with the contraction index slow.
-__host__ __device__ constexpr uint32_t ns_idesc(int N, bool b_mn) {
-  return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
-}
-
 // Write-out of planes.  A warp stages 32 x 32 pieces in the operand buffers (which nothing reads any more) as 32 rows of 64 bytes with the 64-byte swizzle,
 // and TMA stores them; what lies outside the matrix is dropped there.  (Stored from registers, a row of 64 bytes to a lane touches 32 lines per instruction:
 // 6 us for a 256 x 128 tile and its mirror image.)
@@ -192,38 +175,61 @@ constexpr int NS_PIECE = 32 * 64;
 __device__ __forceinline__ uint32_t ns_piece_offset(int row, int col) {      // bytes; col: of halves
   return (uint32_t)(row * 64 + (((col >> 3) ^ (row >> 1)) & 3) * 16 + (col & 7) * 2);
 }
-// a lane's row
-__device__ __forceinline__ void ns_stage_row(uint8_t* piece, int lane, const float (&v)[32]) {      // hi, then lo NS_PIECE bytes on
+template <int NT>
+struct NsTile {
+  static constexpr int A_PLANE = 128 * 128;                  // 128 rows of 64 halves
+  static constexpr int B_PLANE = (NT / 2) * 128;
+  static constexpr int STAGE_BYTES = 2 * A_PLANE + 2 * B_PLANE;
+  static constexpr int STAGES = NT == 256 ? 3 : 4;
+  static constexpr int ADD_BYTES = 8 * 2 * NS_PIECE;         // the first piece of A of each warp, fetched during the product
+  static constexpr int BAR_BYTES = 512;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + ADD_BYTES + BAR_BYTES + 1024;
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a block");
+  // once the operands have been read: two pieces, their mirror images and two planes for each of eight warps, and (NT > 64) two pieces of A each
+  static_assert(8 * 8 * NS_PIECE + (NT > 64 ? 8 * 4 * NS_PIECE : 0) <= STAGES * STAGE_BYTES, "pieces in the operands' place");
+  // B with the contraction index slow: rows of 64 columns (128 bytes), or of the 32 that a block has of a 64-column tile (64 bytes)
+  static constexpr int B_ROW = NT == 64 ? 64 : 128;
+};
+enum : int { NS_WAIT_EMPTY = 101, NS_WAIT_FULL = 102, NS_WAIT_ACC_EMPTY = 103, NS_WAIT_ACC_FULL = 104, NS_WAIT_ADD = 105 };
+
+// Instruction descriptor: IEEE half operands, A row by row (K-major), B row by row or (b_mn) with the contraction index slow.
+__host__ __device__ constexpr uint32_t ns_idesc(int N, bool b_mn) {
+  return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+}
+
+// A lane's row of a piece, hi then lo NS_PIECE bytes on; with mirror also as a column of the piece 2 NS_PIECE on.  Of a piece on the diagonal each value from
+// the diagonal on goes to both places of the piece itself.
+template <bool MIRROR>
+__device__ __forceinline__ void ns_stage(uint8_t* piece, int lane, const float (&v)[32], bool diagonal) {
 #pragma unroll
   for (int j = 0; j < 32; j += 8) {
-    uint32_t hi[4], lo[4];
+    __half h[8], l[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      __half h0, l0, h1, l1;
-      ns_split(v[j + 2 * e], h0, l0);
-      ns_split(v[j + 2 * e + 1], h1, l1);
-      hi[e] = ns_pack(h0, h1);
-      lo[e] = ns_pack(l0, l1);
+    for (int e = 0; e < 8; ++e) ns_split(v[j + e], h[e], l[e]);
+    if (!MIRROR || !diagonal) {
+      uint8_t* at = piece + ns_piece_offset(lane, j);
+      *reinterpret_cast<uint4*>(at) = make_uint4(ns_pack(h[0], h[1]), ns_pack(h[2], h[3]), ns_pack(h[4], h[5]), ns_pack(h[6], h[7]));
+      *reinterpret_cast<uint4*>(at + NS_PIECE) = make_uint4(ns_pack(l[0], l[1]), ns_pack(l[2], l[3]), ns_pack(l[4], l[5]), ns_pack(l[6], l[7]));
     }
-    *reinterpret_cast<uint4*>(piece + ns_piece_offset(lane, j)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(piece + NS_PIECE + ns_piece_offset(lane, j)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  }
-}
-// the same row as a column; of a piece on the diagonal: each value from the diagonal on, to both places
-__device__ __forceinline__ void ns_stage_column(uint8_t* piece, int lane, const float (&v)[32], bool diagonal) {
+    if constexpr (MIRROR) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    __half h, l;
-    ns_split(v[j], h, l);
-    if (!diagonal || j >= lane) {
-      *reinterpret_cast<__half*>(piece + ns_piece_offset(j, lane)) = h;
-      *reinterpret_cast<__half*>(piece + NS_PIECE + ns_piece_offset(j, lane)) = l;
-      if (diagonal) {
-        *reinterpret_cast<__half*>(piece + ns_piece_offset(lane, j)) = h;
-        *reinterpret_cast<__half*>(piece + NS_PIECE + ns_piece_offset(lane, j)) = l;
+      for (int e = 0; e < 8; ++e) {
+        uint8_t* at = piece + ns_piece_offset(j + e, lane);
+        if (!diagonal) {
+          *reinterpret_cast<__half*>(at + 2 * NS_PIECE) = h[e];
+          *reinterpret_cast<__half*>(at + 3 * NS_PIECE) = l[e];
+        } else if (j + e >= lane) {
+          uint8_t* own = piece + ns_piece_offset(lane, j + e);
+          *reinterpret_cast<__half*>(at) = *reinterpret_cast<__half*>(own) = h[e];
+          *reinterpret_cast<__half*>(at + NS_PIECE) = *reinterpret_cast<__half*>(own + NS_PIECE) = l[e];
+        }
       }
     }
   }
+}
+__device__ __forceinline__ void ns_load_piece(uint32_t dst, const CUtensorMap* map, uint32_t bar, int col, int row, int plane) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(col), "r"(row), "r"(plane) : "memory");
 }
 __device__ __forceinline__ void ns_store_piece(const CUtensorMap* map, uint32_t src, int col, int row, int plane) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(col),
@@ -233,20 +239,21 @@ __device__ __forceinline__ void ns_store_piece(const CUtensorMap* map, uint32_t 
 template <int NT, bool B_MN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NS_THREADS, 1)
 ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
-                  const __grid_constant__ NsProduct p) {
+                  const __grid_constant__ CUtensorMap map_add, const __grid_constant__ NsProduct p) {
   using namespace sm100;
   using Tile = NsTile<NT>;
   constexpr int STAGES = Tile::STAGES, ACC = 2, COLS = NT / 2;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t bar_base = smem_base + STAGES * Tile::STAGE_BYTES;
+  const uint32_t add_base = smem_base + STAGES * Tile::STAGE_BYTES, bar_base = add_base + Tile::ADD_BYTES;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
   auto acc_full_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + a); };
   auto acc_empty_bar = [&](int a) { return bar_base + 8u * (2 * STAGES + ACC + a); };
-  uint8_t* tail = smem_gen + STAGES * Tile::STAGE_BYTES + 8 * (2 * STAGES + 2 * ACC);
-  static_assert(8 * (2 * STAGES + 2 * ACC) + 16 <= Tile::BAR_BYTES, "barrier area too small");
+  auto add_bar = [&](int w, int c) { return bar_base + 8u * (2 * STAGES + 2 * ACC + w * (COLS / 32) + c); };      // warp w's piece c of A
+  uint8_t* tail = smem_gen + STAGES * Tile::STAGE_BYTES + Tile::ADD_BYTES + 8 * (2 * STAGES + 2 * ACC + 8 * (COLS / 32));
+  static_assert(8 * (2 * STAGES + 2 * ACC + 8 * (COLS / 32)) + 16 <= Tile::BAR_BYTES, "barrier area too small");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
   volatile int* split_flag = reinterpret_cast<volatile int*>(tail + 12);
@@ -271,8 +278,16 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < ACC; ++a) { mbar_init(acc_full_bar(a), 1); mbar_init(acc_empty_bar(a), 16); }
+    if (EPI == NS_SYMMETRIC)
+      for (int w = 0; w < 8 * (COLS / 32); ++w) mbar_init(add_bar(0, w), 1);
     *abort_flag = 0;
     fence_barrier_init();
+  }
+  if (warp == 2 && elect_one()) {      // (parameters of the launch: not what the kernel before writes)
+    prefetch_tensormap(&map_a);
+    prefetch_tensormap(&map_b);
+    if (EPI != NS_FINAL) prefetch_tensormap(&map_out);
+    if (EPI == NS_SYMMETRIC) prefetch_tensormap(&map_add);
   }
   if (warp == 1) { tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), NS_TMEM_COLS); tmem_relinquish_pair(); }
   tc_fence_before();
@@ -300,7 +315,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           const uint32_t b = dst + 2 * Tile::A_PLANE + plane * Tile::B_PLANE;
           if constexpr (B_MN) {
 #pragma unroll
-            for (int j = 0; j < NT / 128; ++j) tma_load_3d_pair(b + j * (NS_BK * 128), &map_b, leader_full, col + 64 * j, k0, z);
+            for (int j = 0; j < (NT == 256 ? 2 : 1); ++j) tma_load_3d_pair(b + j * (NS_BK * 128), &map_b, leader_full, col + 64 * j, k0, z);
           } else {
             tma_load_3d_pair(b, &map_b, leader_full, k0, col, z);
           }
@@ -337,7 +352,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (int k = 0; k < NS_BK / 16; ++k) {
               if (k * 16 < k_left) {
                 const uint64_t ad = make_smem_desc(ap + k * 32, 16u, 1024u, 2u);
-                const uint64_t bd = B_MN ? make_smem_desc(bp + k * 2048, NS_BK * 128, 1024u, 2u) : make_smem_desc(bp + k * 32, 16u, 1024u, 2u);
+                const uint64_t bd = B_MN ? make_smem_desc(bp + k * 16 * Tile::B_ROW, NS_BK * Tile::B_ROW, 8 * Tile::B_ROW, NT == 64 ? 4u : 2u) : make_smem_desc(bp + k * 32, 16u, 1024u, 2u);
                 umma_ss_pair<0>(d_tmem, ad, bd, idesc, accumulate);
                 accumulate = 1;
               }
@@ -354,11 +369,31 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     // ---------------------------------------------------------- epilogue (both blocks)
     const int q = warp & 3, h = (warp - 2) >> 2;      // lanes of tensor memory that this warp may read, half of the columns
     const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
-    const int r = tile_m * 256 + (int)rank * 128 + q * 32 + lane, c0 = tile_n * NT + h * COLS;
+    const int c0 = tile_n * NT + h * COLS;
     float acc[COLS];
 #pragma unroll
     for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
     bool ok = true;
+    // A's pieces that this warp adds: the first one into a place of its own at once, the others into the operands' place later.
+    const int row0 = tile_m * 256 + (int)rank * 128 + q * 32;
+    auto piece_counts = [&](int c) {      // (the warp as one) is this piece inside, and not below the diagonal, where it is the mirror image of another
+      const int col = c0 + c * 32;
+      return col < p.cols && row0 < p.rows && (EPI != NS_SYMMETRIC || col + 31 >= row0);
+    };
+    constexpr int ADD_PLACE = 8 * 8 * NS_PIECE;      // behind the staging areas
+    auto add_at = [&](int c) {      // byte offset from smem_base
+      return c == 0 ? (uint32_t)(STAGES * Tile::STAGE_BYTES + (warp - 2) * (2 * NS_PIECE)) : (uint32_t)(ADD_PLACE + ((warp - 2) * 2 + (c & 1)) * (2 * NS_PIECE));
+    };
+    auto fetch_add = [&](int c) {
+      if (piece_counts(c) && elect_one()) {
+        const uint32_t bar = add_bar(warp - 2, c);
+        mbar_arrive_expect_tx(bar, 2 * NS_PIECE);
+        ns_load_piece(smem_base + add_at(c), &map_add, bar, c0 + c * 32, row0, mat);
+        ns_load_piece(smem_base + add_at(c) + NS_PIECE, &map_add, bar, c0 + c * 32, row0, p.count + mat);
+      }
+      __syncwarp();
+    };
+    if (EPI == NS_SYMMETRIC && p.add) fetch_add(0);
     for (int a = 0; a < n_acc; ++a) {
       const int buf = a % ACC;
       if (!mbar_wait_warp(acc_full_bar(buf), (uint32_t)(a / ACC) & 1u, abort_flag, p.dev_status, NS_WAIT_ACC_FULL)) { ok = false; break; }
@@ -376,6 +411,8 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int j = 0; j < 32; ++j) acc[c * 32 + j] += __uint_as_float(v[j]);
       }
     }
+    if (EPI == NS_SYMMETRIC && p.add && piece_counts(0))      // (landed before anybody leaves, written out or not)
+      ok = mbar_wait_warp(add_bar(warp - 2, 0), 0, abort_flag, p.dev_status, NS_WAIT_ADD) && ok;
     bool write = true;
     if (p.splits > 1) {      // (all eight warps of the block, whatever their waits said)
       const size_t tiles = (size_t)p.units * p.count, mine = ((size_t)unit * 2 + rank) * 8 + (warp - 2);
@@ -406,15 +443,23 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (EPI == NS_FINAL && *reinterpret_cast<volatile unsigned int*>(p.dev_status) != 0u) write = false;      // an earlier product may have given up
     if (ok && write) {
       // A warp's 32 x 32 pieces; lanes hold rows.
-      const int row0 = tile_m * 256 + (int)rank * 128 + q * 32;
+      if constexpr (EPI == NS_SYMMETRIC && COLS > 32) {
+        if (p.add) {
+          fetch_add(1);
+          if constexpr (COLS > 64) fetch_add(2);
+        }
+      }
       uint8_t* const staging = smem_gen + (warp - 2) * (8 * NS_PIECE);
       const uint32_t staging_s = smem_base + (uint32_t)(warp - 2) * (8 * NS_PIECE);
-      static_assert(8 * 8 * NS_PIECE <= STAGES * Tile::STAGE_BYTES, "two pieces, their mirror images and two planes for each of eight warps");
       int used = 0;      // pieces staged
 #pragma unroll
       for (int c = 0; c < COLS / 32; ++c) {
         const int col = c0 + c * 32;
-        if (col >= p.cols || row0 >= p.rows) continue;      // (the warp as one)
+        if (EPI == NS_SYMMETRIC && c == 2 && p.add) {      // piece 1 has been read, or does not count: its place is free
+          __syncwarp();
+          fetch_add(3);
+        }
+        if (!piece_counts(c)) continue;
         float v[32];
         if constexpr (EPI == NS_FINAL) {
           // along the lanes in memory: rows of the result by way of shared memory, columns (a transposed result) as they are
@@ -461,27 +506,22 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
           }
         } else {
-          const size_t mat0 = (size_t)mat * p.rows, plane = (size_t)p.count * p.rows * p.ld;
-          if (EPI == NS_SYMMETRIC && col + 31 < row0) continue;      // below the diagonal: the mirror image of another piece
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = acc[c * 32 + j] * NS_UNSCALE;      // 2^12 of the value
           const bool diagonal = EPI == NS_SYMMETRIC && col == row0;
           if constexpr (EPI == NS_SYMMETRIC) {
             if (p.add) {
-              if (r < p.rows) {
-                const __half* at = p.add + (mat0 + r) * p.ld + col;
+              if (!mbar_wait_warp(add_bar(warp - 2, c), 0, abort_flag, p.dev_status, NS_WAIT_ADD)) break;
+              const uint8_t* from = smem_gen + add_at(c);
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                  if (col + j < p.cols) {
-                    const uint4 h4 = *reinterpret_cast<const uint4*>(at + j), l4 = *reinterpret_cast<const uint4*>(at + plane + j);
-                    const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+              for (int j = 0; j < 32; j += 8) {      // (zeros outside the matrix)
+                const uint4 h4 = *reinterpret_cast<const uint4*>(from + ns_piece_offset(lane, j)), l4 = *reinterpret_cast<const uint4*>(from + NS_PIECE + ns_piece_offset(lane, j));
+                const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                      const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hw[e])), l = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
-                      v[j + 2 * e] = fmaf(NS_C, v[j + 2 * e], NS_B * (h.x + l.x));
-                      v[j + 2 * e + 1] = fmaf(NS_C, v[j + 2 * e + 1], NS_B * (h.y + l.y));
-                    }
-                  }
+                for (int e = 0; e < 4; ++e) {
+                  const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hw[e])), l = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
+                  v[j + 2 * e] = fmaf(NS_C, v[j + 2 * e], NS_B * (h.x + l.x));
+                  v[j + 2 * e + 1] = fmaf(NS_C, v[j + 2 * e + 1], NS_B * (h.y + l.y));
                 }
               }
               if (diagonal) {
@@ -497,12 +537,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
             __syncwarp();
           }
-          if (diagonal) {
-            ns_stage_column(piece, lane, v, true);
-          } else {
-            ns_stage_row(piece, lane, v);
-            if (EPI == NS_SYMMETRIC) ns_stage_column(piece + 2 * NS_PIECE, lane, v, false);
-          }
+          ns_stage<EPI == NS_SYMMETRIC>(piece, lane, v, diagonal);
           fence_async_smem();
           __syncwarp();
           if (lane == 0) {
