@@ -95,17 +95,25 @@ static pe_status_t ns_map(CUtensorMap* map, const void* base, int planes, int ro
              ? PE_OK : PE_ERR_CUDA;
 }
 
+// Lets `kernel` use `smem` bytes of shared memory on the current device; ready: the devices where it may already.
+template <typename Kernel>
+static pe_status_t allow_smem(Kernel kernel, std::atomic<unsigned long long> (&ready)[MAX_DEVICES / 64], int smem) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) { cudaGetLastError(); return PE_ERR_CUDA; }
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (ready[dev >> 6].load(std::memory_order_acquire) & bit) return PE_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  ready[dev >> 6].fetch_or(bit, std::memory_order_release);
+  return PE_OK;
+}
+static bool ns_is_small(const NsLayout& l) { return l.n <= NS_SMALL_N && l.m <= NS_SMALL_M; }
+
 template <int NT, bool B_MN, int EPI>
 static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const CUtensorMap& add, NsProduct p, cudaStream_t st) {
-  static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];      // devices whose kernel attribute is set
+  static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];
   auto kernel = ns_product_kernel<NT, B_MN, EPI>;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-  const unsigned long long bit = 1ull << (dev & 63);
-  if (!(ready[dev >> 6].load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NsTile<NT>::SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-    ready[dev >> 6].fetch_or(bit, std::memory_order_release);
-  }
+  const pe_status_t rc = allow_smem(kernel, ready, NsTile<NT>::SMEM_BYTES);
+  if (rc != PE_OK) return rc;
   p.tiles_n = (p.cols + NT - 1) / NT;
   return launch_dependent(kernel, dim3((unsigned)(2ll * p.units * p.count * p.splits)), NS_THREADS, NsTile<NT>::SMEM_BYTES, st, a, b, out, add, p);
 }
@@ -121,6 +129,14 @@ static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, cons
 // The iteration on what `s` describes; `out` holds the last product's output side.
 static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, int rows, int cols, int steps, const NsProduct& out, char* ws, cudaStream_t st) {
   const NsLayout l = ns_layout(count, rows, cols);
+  if (ns_is_small(l)) {
+    static std::atomic<unsigned long long> ready[MAX_DEVICES / 64];
+    const int most = (NS_SMALL_N * ns_small_ld(NS_SMALL_M) + 2 * NS_SMALL_N * NS_SMALL_LD) * (int)sizeof(float);
+    const pe_status_t rc = allow_smem(ns_small_kernel, ready, most);
+    if (rc != PE_OK) return rc;
+    const int smem = (NS_SMALL_N * ns_small_ld(l.m) + 2 * NS_SMALL_N * NS_SMALL_LD) * (int)sizeof(float);
+    return launch_dependent(ns_small_kernel, dim3(count), NS_SMALL_THREADS, smem, st, s, out.to, l.n, l.m, l.tall, steps);
+  }
   double* norms = reinterpret_cast<double*>(ws + l.norms);
   __half* x[2] = {reinterpret_cast<__half*>(ws + l.x[0]), reinterpret_cast<__half*>(ws + l.x[1])};
   __half *const a = reinterpret_cast<__half*>(ws + l.a), *const q = reinterpret_cast<__half*>(ws + l.q);
@@ -178,7 +194,7 @@ static pe_status_t orthogonalize_impl(const void* G, int bf16, int count, int ro
   NsSource s = {};
   s.given = G; s.bf16 = bf16;
   NsProduct p = {};
-  p.result = out; p.out_bf16 = bf16; p.transposed = rows > cols;
+  p.to.result = out; p.to.out_bf16 = bf16; p.transposed = rows > cols;
   return newton_schulz(di, s, count, rows, cols, steps, p, static_cast<char*>(workspace), st);
 }
 
@@ -217,7 +233,7 @@ pe_status_t muon_step(float* theta, void* theta_lp, float* m, const float* sum_g
   NsSource s = {};
   s.m = m; s.sum_g = sum_g; s.grad_scale = (float)((double)grad_scale / (double)B); s.beta = beta; s.nesterov = nesterov != 0;
   NsProduct p = {};
-  p.theta = theta; p.theta_lp = static_cast<__nv_bfloat16*>(theta_lp); p.step = lr * update_scale; p.wd = weight_decay; p.transposed = rows > cols;
+  p.to.theta = theta; p.to.theta_lp = static_cast<__nv_bfloat16*>(theta_lp); p.to.step = lr * update_scale; p.to.wd = weight_decay; p.transposed = rows > cols;
   return newton_schulz(di, s, count, rows, cols, steps, p, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream));
 }
 

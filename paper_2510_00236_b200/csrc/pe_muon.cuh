@@ -139,6 +139,153 @@ ns_init_kernel(NsSource s, int n, int m, int ld, int tall, int tiles_m, const do
   }
 }
 
+// ---------------------------------------------------------------- small matrices
+// n <= 64 and m <= 128: one block takes a matrix through all of it, in fp32 in shared memory.  The tensor-core path is 17 launches of 4.4 us there, whatever the
+// size; this takes one (64 x 64: 75 us by the products, 38 us here; 64 x 128: 79 and 58; 64 x 256: 83 and 101).
+constexpr int NS_SMALL_N = 64, NS_SMALL_M = 128;
+constexpr int NS_SMALL_THREADS = 256;
+constexpr int NS_SMALL_LD = NS_SMALL_N + 4;               // rows of A and Q
+struct NsResult {
+  void* result;                 // bf16 or fp32, or NULL and
+  int out_bf16;
+  float* theta;                 // theta <- theta - step X - wd theta
+  __nv_bfloat16* theta_lp;
+  float step, wd;
+};
+__host__ __device__ constexpr int ns_small_ld(int m) { return (m + 31) / 32 * 32 + 4; }      // 4 words past a multiple of 32: rows start 4 banks apart
+// out[i][j] = rows ty + 16 i of a times rows tx + 16 j of b, over k (a multiple of 4); sums of even and odd terms side by side
+__device__ __forceinline__ void ns_small_rows(const float* a, const float* b, int ld, int k, int ty, int tx, float (&out)[4][4]) {
+  uint64_t acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0ull;
+#pragma unroll 2
+  for (int q = 0; q < k; q += 4) {
+    ulonglong2 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = *reinterpret_cast<const ulonglong2*>(a + (ty + 16 * i) * ld + q);
+      y[i] = *reinterpret_cast<const ulonglong2*>(b + (tx + 16 * i) * ld + q);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = sm100::f32x2_fma(x[i].x, y[j].x, acc[i][j]);
+        acc[i][j] = sm100::f32x2_fma(x[i].y, y[j].y, acc[i][j]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      sm100::f32x2_unpack(acc[i][j], lo, hi);
+      out[i][j] = lo + hi;
+    }
+}
+__global__ void __launch_bounds__(NS_SMALL_THREADS)
+ns_small_kernel(NsSource s, NsResult o, int n, int m, int tall, int steps) {
+  sm100::griddep_launch_dependents();
+  sm100::griddep_wait();
+  extern __shared__ __align__(16) float ns_small[];
+  __shared__ double warp_sum[NS_SMALL_THREADS / 32];
+  const int ld = ns_small_ld(m), width = ld - 4, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  float *X = ns_small, *A = X + NS_SMALL_N * ld, *Q = A + NS_SMALL_N * NS_SMALL_LD;
+  const long long base = (long long)blockIdx.x * n * m;
+  for (int i = threadIdx.x; i < NS_SMALL_N * ld; i += NS_SMALL_THREADS) X[i] = 0.f;
+  __syncthreads();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < n * m; i += NS_SMALL_THREADS) {
+    float v;
+    if (s.given) {
+      v = ns_source_value(s, base + i);
+    } else {
+      const float g = s.sum_g[base + i] * s.grad_scale, mom = fmaf(s.beta, s.m[base + i], (1.f - s.beta) * g);
+      s.m[base + i] = mom;
+      v = s.nesterov ? fmaf(s.beta, mom, (1.f - s.beta) * g) : mom;
+    }
+    sum += (double)v * (double)v;
+    X[tall ? (i % n) * ld + i / n : (i / m) * ld + i % m] = v;
+  }
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  sum = 0.0;
+  for (int w = 0; w < NS_SMALL_THREADS / 32; ++w) sum += warp_sum[w];
+  const double inv = sum == 0.0 ? 0.0 : 1.0 / sqrt(sum);
+  for (int i = threadIdx.x; i < NS_SMALL_N * width; i += NS_SMALL_THREADS) {
+    float* x = X + i / width * ld + i % width;
+    *x = (float)((double)*x * inv);
+  }
+  __syncthreads();
+  for (int k = 0; k < steps; ++k) {
+    float c[4][4];
+    ns_small_rows(X, X, ld, width, ty, tx, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) A[(ty + 16 * i) * NS_SMALL_LD + tx + 16 * j] = c[i][j];
+    __syncthreads();
+    ns_small_rows(A, A, NS_SMALL_LD, NS_SMALL_N, ty, tx, c);      // (A is symmetric: its rows are its columns)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = (ty + 16 * i) * NS_SMALL_LD + tx + 16 * j;
+        Q[at] = fmaf(NS_C, c[i][j], fmaf(NS_B, A[at], ty + 16 * i == tx + 16 * j ? NS_A : 0.f));
+      }
+    __syncthreads();
+    for (int c0 = 0; c0 < width; c0 += 64) {      // 64 columns of Q X at a time: rows ty + 16 i, columns c0 + 4 tx ..
+      uint64_t acc[4][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = 0ull;
+      const bool in = c0 + 4 * tx < width;
+      if (in) {
+#pragma unroll 2
+        for (int q = 0; q < NS_SMALL_N; q += 4) {
+          float4 w[4];
+          ulonglong2 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            w[i] = *reinterpret_cast<const float4*>(Q + (ty + 16 * i) * NS_SMALL_LD + q);
+            x[i] = *reinterpret_cast<const ulonglong2*>(X + (q + i) * ld + c0 + 4 * tx);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float f[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint64_t ff = sm100::f32x2_pack(f[e], f[e]);
+              acc[i][0] = sm100::f32x2_fma(ff, x[e].x, acc[i][0]);
+              acc[i][1] = sm100::f32x2_fma(ff, x[e].y, acc[i][1]);
+            }
+          }
+        }
+      }
+      __syncthreads();      // these columns have been read
+      if (in) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<ulonglong2*>(X + (ty + 16 * i) * ld + c0 + 4 * tx) = make_ulonglong2(acc[i][0], acc[i][1]);
+      }
+    }
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < n * m; i += NS_SMALL_THREADS) {
+    const float v = X[tall ? (i % n) * ld + i / n : (i / m) * ld + i % m];
+    if (o.result) {
+      if (o.out_bf16) static_cast<__nv_bfloat16*>(o.result)[base + i] = __float2bfloat16_rn(v);
+      else static_cast<float*>(o.result)[base + i] = v;
+    } else {
+      const float th = o.theta[base + i], next = th - o.step * v - o.wd * th;
+      o.theta[base + i] = next;
+      if (o.theta_lp) o.theta_lp[base + i] = __float2bfloat16_rn(next);
+    }
+  }
+}
+
 // ---------------------------------------------------------------- products
 // A pair of thread blocks contracts one 256 x NT tile of one matrix.  Warp 0 of each block feeds its share of the operands by TMA (both
 // planes of 64 values of the contraction index per stage), warp 1 of the leader issues the MMAs, eight warps per block add up what is in
@@ -158,11 +305,8 @@ struct NsProduct {
   unsigned int* counters;        // [units * count][2], zero before and after a product
   int add;                       // NS_SYMMETRIC: 0, or 1: the result is a I + b A + c (product), A by map_add
   // NS_FINAL: the result itself, [rows, cols] per matrix, or transposed: [cols, rows]
-  int transposed, out_bf16;
-  void* result;                  // as given, or NULL and
-  float* theta;                  // theta <- theta - step X - wd theta
-  __nv_bfloat16* theta_lp;
-  float step, wd;
+  int transposed;
+  NsResult to;
   unsigned int* dev_status;
 };
 constexpr int NS_THREADS = 320;
@@ -478,8 +622,8 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           const int n_slow = (p.transposed ? p.cols : p.rows) - slow0, n_fast = p.transposed ? p.rows : p.cols;
           const size_t base = (size_t)mat * p.rows * p.cols + (size_t)slow0 * n_fast + fast;
           if (fast < n_fast) {
-            if (!p.result) {
-              float* th = p.theta + base;
+            if (!p.to.result) {
+              float* th = p.to.theta + base;
 #pragma unroll
               for (int j0 = 0; j0 < 32; j0 += 8) {      // eight loads in flight
                 float old[8];
@@ -488,18 +632,18 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                   if (j0 + j < n_slow) {
-                    const float next = old[j] - p.step * v[j0 + j] - p.wd * old[j];
+                    const float next = old[j] - p.to.step * v[j0 + j] - p.to.wd * old[j];
                     th[(size_t)(j0 + j) * n_fast] = next;
-                    if (p.theta_lp) p.theta_lp[base + (size_t)(j0 + j) * n_fast] = __float2bfloat16_rn(next);
+                    if (p.to.theta_lp) p.to.theta_lp[base + (size_t)(j0 + j) * n_fast] = __float2bfloat16_rn(next);
                   }
               }
-            } else if (p.out_bf16) {
-              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.result) + base;
+            } else if (p.to.out_bf16) {
+              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.to.result) + base;
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (j < n_slow) to[(size_t)j * n_fast] = __float2bfloat16_rn(v[j]);
             } else {
-              float* to = static_cast<float*>(p.result) + base;
+              float* to = static_cast<float*>(p.to.result) + base;
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (j < n_slow) to[(size_t)j * n_fast] = v[j];
