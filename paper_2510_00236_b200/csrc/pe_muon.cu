@@ -159,7 +159,6 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   NsProduct p = out;
   p.count = count;
   p.dev_status = di->status_ptr;
-  p.chunk = 2;
   p.partial = reinterpret_cast<float*>(ws + l.partial);
   p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
   for (int k = 0; k < steps; ++k) {

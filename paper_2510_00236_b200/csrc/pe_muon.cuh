@@ -292,14 +292,15 @@ ns_small_kernel(NsSource s, NsResult o, int n, int m, int tall, int steps) {
 // tensor memory and write the tile out.
 //
 // The tensor cores add to their fp32 accumulator by truncation, which pulls long sums of one sign (the diagonal of A) towards zero, a
-// little per instruction.  So an accumulator takes `chunk` stages, the small cross terms before hi hi, and the chunks are added
-// up in registers, rounded to nearest: two accumulators in turn, drained while the other one fills.
+// little per instruction.  So an accumulator takes one stage, the small cross terms before hi hi, and the stages are added
+// up in registers, rounded to nearest: two accumulators in turn, drained while the other one fills.  (8192 x 2048: 1.4e-6 off the exact polynomial and
+// 1526 us; two stages to an accumulator 3.1e-6 and 1470, all of them 5.7e-5 and 1410.  fp32 products in the same steps are 1.3e-6 off.)
 enum : int { NS_SYMMETRIC = 0, NS_PLANES = 1, NS_FINAL = 2 };
 struct NsProduct {
   int rows, cols, k;             // of the product: [rows, cols], contracted over k
   int tiles_n;                   // column tiles; NS_SYMMETRIC: those that touch the upper triangle are worked on
   int units;                     // tiles per matrix
-  int count, chunk;
+  int count;
   int splits;                    // slices of the contraction index, each a pair's; the last one done adds the partial tiles up in their order
   float* partial;                // [splits][units * count][2][8 warps][NT / 2][32], where there are several
   unsigned int* counters;        // [units * count][2], zero before and after a product
@@ -417,7 +418,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     tile_n -= tile_m * p.tiles_n;
   }
   const int all_stages = (p.k + NS_BK - 1) / NS_BK, stage0 = (int)((long long)all_stages * slice / p.splits);
-  const int stages = (int)((long long)all_stages * (slice + 1) / p.splits) - stage0, n_acc = (stages + p.chunk - 1) / p.chunk;
+  const int stages = (int)((long long)all_stages * (slice + 1) / p.splits) - stage0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -477,17 +478,15 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       uint32_t ph = 0;
       bool ok = true;
       for (int ks = 0; ks < stages && ok; ++ks) {
-        const int a = ks / p.chunk, in_chunk = ks - a * p.chunk, buf = a % ACC;
-        if (in_chunk == 0) {
-          if (!mbar_wait_warp(acc_empty_bar(buf), ((uint32_t)(a / ACC) & 1u) ^ 1u, abort_flag, p.dev_status, NS_WAIT_ACC_EMPTY, strict)) { ok = false; break; }
-          tc_fence_after();
-        }
+        const int buf = ks % ACC;
+        if (!mbar_wait_warp(acc_empty_bar(buf), ((uint32_t)(ks / ACC) & 1u) ^ 1u, abort_flag, p.dev_status, NS_WAIT_ACC_EMPTY, strict)) { ok = false; break; }
+        tc_fence_after();
         if (!mbar_wait_warp(full_bar(s), ph, abort_flag, p.dev_status, NS_WAIT_FULL, strict)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
           const uint32_t d_tmem = tmem_base + (uint32_t)(buf * NT);
           const uint32_t a_src = smem_base + s * Tile::STAGE_BYTES, b_src = a_src + 2 * Tile::A_PLANE;
-          uint32_t accumulate = in_chunk > 0;
+          uint32_t accumulate = 0;
           const int k_left = p.k - (stage0 + ks) * NS_BK;
 #pragma unroll
           for (int term = 0; term < 3; ++term) {        // hi lo, lo hi, hi hi
@@ -503,7 +502,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
           }
           umma_commit_pair(empty_bar(s));
-          if (ks == stages - 1 || in_chunk == p.chunk - 1) umma_commit_pair(acc_full_bar(buf));
+          umma_commit_pair(acc_full_bar(buf));
         }
         __syncwarp();
         if (++s == STAGES) { s = 0; ph ^= 1u; }
@@ -538,7 +537,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       __syncwarp();
     };
     if (EPI == NS_SYMMETRIC && p.add) fetch_add(0);
-    for (int a = 0; a < n_acc; ++a) {
+    for (int a = 0; a < stages; ++a) {
       const int buf = a % ACC;
       if (!mbar_wait_warp(acc_full_bar(buf), (uint32_t)(a / ACC) & 1u, abort_flag, p.dev_status, NS_WAIT_ACC_FULL)) { ok = false; break; }
       tc_fence_after();

@@ -236,35 +236,42 @@ __device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, c
   return 0;
 }
 
-// A thread's 8 features of a row in shared memory, as pairs: its first vector is at byte `at`, the next ones G vectors further on; `fill` where a feature is
-// out of range (vectors of 8: the caller leaves such threads out).
+// A thread's 8 features of a row in shared memory, as pairs: vector i is `offset[i]` bytes past byte `at`.  Vectors that are out of range have the offset of the
+// first one (norm_offsets): what they hold then is weighted with zero, or not written, by the caller.  Threads whose first vector is out of range are left out.
 template <typename T, int E>
-__device__ __forceinline__ void norm_row_pairs(const uint8_t* shared, uint32_t at, int G, int t, int cols, float fill, uint64_t (&o)[NORM_COLS / 2]) {
+__device__ __forceinline__ void norm_row_pairs(const uint8_t* shared, uint32_t at, const uint32_t (&offset)[NORM_COLS / E], uint64_t (&o)[NORM_COLS / 2]) {
   constexpr int NV = NORM_COLS / E;
   float f[NV][E];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const uint8_t* q = shared + (at + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)));
+    const uint8_t* q = shared + (at + offset[i]);
     if constexpr (E == 8) {
       const uint4 v = *reinterpret_cast<const uint4*>(q);
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int h = 0; h < 4; ++h) { f[i][2 * h] = __uint_as_float(w[h] << 16); f[i][2 * h + 1] = __uint_as_float(w[h] & 0xffff0000u); }
+    } else if constexpr (E == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(q);
+      f[i][0] = v.x; f[i][1] = v.y; f[i][2] = v.z; f[i][3] = v.w;
     } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) f[i][e] = fill;
-      if ((i * G + t) * E < cols) {
-        if constexpr (E == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(q);
-          f[i][0] = v.x; f[i][1] = v.y; f[i][2] = v.z; f[i][3] = v.w;
-        } else {
-          f[i][0] = (float)*reinterpret_cast<const T*>(q);
-        }
-      }
+      f[i][0] = (float)*reinterpret_cast<const T*>(q);
     }
   }
 #pragma unroll
   for (int j = 0; j < NORM_COLS / 2; ++j) o[j] = sm100::f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
+}
+// The vectors' offsets, and 1 or 0 for the features: in range or not.
+template <typename T, int E>
+__device__ __forceinline__ void norm_offsets(int G, int t, int cols, uint32_t (&offset)[NORM_COLS / E], uint64_t (&in)[NORM_COLS / 2]) {
+  float f[NORM_COLS / E];
+#pragma unroll
+  for (int i = 0; i < NORM_COLS / E; ++i) {
+    const bool inside = (i * G + t) * E < cols;
+    offset[i] = inside ? (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)) : 0u;
+    f[i] = inside ? 1.f : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < NORM_COLS / 2; ++j) in[j] = sm100::f32x2_pack(f[2 * j / E], f[(2 * j + 1) / E]);
 }
 
 // s / d, with a reciprocal and a correction by the remainder: the quotient itself where it is a float, so that the mean of equal values is that value.
@@ -437,7 +444,10 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
       b2[j] = f32x2_pack(h[2 * j / E][2 * j % E], h[(2 * j + 1) / E][(2 * j + 1) % E]);
     }
   }
-  const bool active = E < 8 || t * E < d;
+  const bool active = t * E < d;
+  uint32_t offset[NV];
+  uint64_t inside[P];
+  norm_offsets<T, E>(G, t, d, offset, inside);
   const float fd = (float)d, inv_d = 1.f / fd;
   int turn = 0, sl = 0;
   uint32_t phase = 0;
@@ -452,7 +462,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     __syncwarp();
     const uint32_t first = at + (E > 1 ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(x + (r0 + row0) * d) & 15));
     // rows behind the last one hold what was there before: their results are not written
-    auto pairs = [&](int k, float fill, uint64_t (&o)[P]) { norm_row_pairs<T, E>(smem, first + k * row_bytes, G, t, d, fill, o); };
+    auto pairs = [&](int k, uint64_t (&o)[P]) { norm_row_pairs<T, E>(smem, first + k * row_bytes, offset, o); };
     float mu[R], q[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) mu[k] = q[k] = 0.f;
@@ -461,9 +471,9 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
 #pragma unroll
         for (int k = 0; k < R; ++k) {
           uint64_t f[P], s2 = 0ull;
-          pairs(k, 0.f, f);
+          pairs(k, f);
 #pragma unroll
-          for (int j = 0; j < P; ++j) s2 = f32x2_add(s2, f[j]);
+          for (int j = 0; j < P; ++j) s2 = E == 8 ? f32x2_add(s2, f[j]) : f32x2_fma(f[j], inside[j], s2);
           float lo, hi;
           f32x2_unpack(s2, lo, hi);
           mu[k] = lo + hi;
@@ -475,12 +485,12 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         uint64_t f[P], s2 = 0ull;
-        pairs(k, mu[k], f);      // (features out of range: no deviation)
+        pairs(k, f);
         const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
           const uint64_t c = RMS ? f[j] : f32x2_add(f[j], m2);
-          s2 = f32x2_fma(c, c, s2);
+          s2 = f32x2_fma(E == 8 ? c : f32x2_mul(c, inside[j]), c, s2);
         }
         float lo, hi;
         f32x2_unpack(s2, lo, hi);
@@ -500,7 +510,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     }
     auto write_row = [&](int k) {
       uint64_t f[P];
-      pairs(k, 0.f, f);
+      pairs(k, f);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(q[k], q[k]);
       float o[NV][E];
 #pragma unroll
@@ -787,15 +797,26 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   int held_end = chunk;      // rows up to here are held
   float mu[R], rs[R];
   float2 means[SUMMED ? 1 : R];
-  const bool active = E < 8 || t * E < cols;      // a thread with features (of vectors of less than 8, some may be out of range)
+  const bool active = t * E < cols;      // a thread with features
+  uint32_t offset[NV];
+  uint64_t inside[P];
+  norm_offsets<T, E>(G, t, cols, offset, inside);
+#pragma unroll
+  for (int j = 0; j < P; ++j)
+    if constexpr (E < 8) gain[j] = f32x2_mul(gain[j], inside[j]);      // features out of range have no part in the row's means
   // this thread's features of row k of the slot, as pairs
   auto pairs = [&](uint32_t tensor_at, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
-    if constexpr (E == 1) tensor_at += (uint32_t)(reinterpret_cast<uintptr_t>(tensor + (WHOLE ? row : row + k) * d + col0) & 15);
-    norm_row_pairs<T, E>(smem, tensor_at + k * row_bytes, G, t, cols, 0.f, o);
+    if constexpr (E == 1 && !WHOLE) tensor_at += (uint32_t)(reinterpret_cast<uintptr_t>(tensor + (row + k) * d + col0) & 15);
+    norm_row_pairs<T, E>(smem, tensor_at + k * row_bytes, offset, o);
   };
   for (int b = 0; b < turns; ++b) {
     const int row0 = b * R;
-    const uint32_t at_y = at + (uint32_t)slot;
+    uint32_t at_x = at, at_y = at + (uint32_t)slot;
+    if constexpr (E == 1 && WHOLE) {      // where in a 16-byte word the rows begin
+      const uint32_t skip = (uint32_t)((r0 + row0) * d) * (uint32_t)sizeof(T);
+      at_x += (skip + (uint32_t)reinterpret_cast<uintptr_t>(x)) & 15;
+      at_y += (skip + (uint32_t)reinterpret_cast<uintptr_t>(dy)) & 15;
+    }
     if (waits && row0 < n_rows) waits = mbar_wait_bounded(bars + 8 * sl, phase, &abort_flag, p.dev_status, NORM_WAIT_ROWS, strict);
     __syncwarp();
 #pragma unroll
@@ -815,7 +836,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
     auto sums_of = [&](int k) {
       uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
-      pairs(at, x, r0 + row0, k, fx);
+      pairs(at_x, x, r0 + row0, k, fx);
       pairs(at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
 #pragma unroll
@@ -916,7 +937,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
         if constexpr (!RMS) k0 = -rs[k] * means[k].y;
       }
       uint64_t fx[P], fy[P];
-      pairs(at, x, r0 + row0, k, fx);
+      pairs(at_x, x, r0 + row0, k, fx);
       pairs(at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
       float o[NV][E];
