@@ -163,7 +163,7 @@ static pe_status_t launch_rows(const T* x, const T* dy, T* dx, const NormBackwar
   return rc != PE_OK ? rc : launch_dependent(kernel, dim3(p.blocks, p.slabs), p.G * p.groups, smem, st, x, dy, dx, a);
 }
 template <typename T, int E, bool RMS, int KINDS>
-static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward a, BackwardPlan& p, char* ws, cudaStream_t st) {
+static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward& a, BackwardPlan& p, char* ws, cudaStream_t st) {
   const int threads = p.G * p.groups;
   // the ring and its barriers, and in the same place later the workers' elements
   const size_t slot = norm_slot_bytes(norm_rows<T>(), p.mode == NORM_WHOLE ? a.d : p.G * NORM_COLS, sizeof(T), p.mode == NORM_WHOLE);
@@ -242,7 +242,8 @@ static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, con
   if (!aligned(workspace, 256)) return PE_ERR_ALIGN;
   NormBackward a = {};
   a.gain = gain; a.mean = mean; a.rstd = rstd; a.offsets = packed ? offsets : nullptr;
-  a.wide = aligned(gain, 16); a.rows = rows; a.B = B; a.T = T_; a.d = d; a.phi = (int)phi;
+  a.wide = aligned(gain, 16); a.rows = rows; a.B = B; a.T = T_; a.d = d; a.phi = (int)phi; a.accumulate = accumulate;
+  a.sums[0] = gain_sum; a.sums[1] = gain_stat; a.sums[2] = bias_sum; a.sums[3] = bias_stat;
   constexpr int E = 16 / (int)sizeof(T);
   char* ws = static_cast<char*>(workspace);
   const bool vec = d % E == 0 && aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16);
@@ -253,14 +254,10 @@ static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, con
   };
   rc = vec ? with(std::integral_constant<int, E>{}) : with(std::integral_constant<int, 1>{});
   if (rc != PE_OK || (!bias && !gain_sum && !gain_stat)) return rc;
-  const float* parts = reinterpret_cast<const float*>(ws);
-  const int* ends = reinterpret_cast<const int*>(ws + p.ends_at);
+  if (p.mode == NORM_WHOLE && p.blocks == 1) return PE_OK;      // (the one block has written them)
   const dim3 grid((unsigned)(kinds * ((d + 31) / 32)));
-  if (bias)
-    return launch_dependent(norm_join_kernel<2>, grid, 32 * NORM_JOIN_WARPS, 0, st, parts, ends, p.blocks, d, (int)phi, accumulate, gain_sum, gain_stat,
-                            bias_sum, bias_stat);
-  return launch_dependent(norm_join_kernel<1>, grid, 32 * NORM_JOIN_WARPS, 0, st, parts, ends, p.blocks, d, (int)phi, accumulate, gain_sum, gain_stat,
-                          bias_sum, bias_stat);
+  return bias ? launch_dependent(norm_join_kernel<2>, grid, 32 * NORM_JOIN_WARPS, 0, st, a, p.blocks)
+              : launch_dependent(norm_join_kernel<1>, grid, 32 * NORM_JOIN_WARPS, 0, st, a, p.blocks);
 }
 
 }  // namespace pe

@@ -617,6 +617,8 @@ struct NormBackward {
   long long rows;                       // rows of the tensors
   int B, T, d, phi, G;                  // G threads per row
   int wide;                             // gain is 16-byte aligned
+  float* sums[4];                       // gain_sum, gain_stat, bias_sum, bias_stat, or NULL
+  int accumulate;
   int cluster;                          // NORM_CLUSTER: blocks of a cluster
   float* parts;                         // [blocks][NORM_PARTS][kinds][d]; a block's element
   int* ends;                            // [blocks]: whether an example ends in the block's rows
@@ -624,6 +626,14 @@ struct NormBackward {
   unsigned int* dev_status;
   const float2* row_means;              // of each row: (mean(w xh), mean(w)), where a kernel before this one found them
 };
+
+// The sums over all examples from the element of all rows: what came before the first end is an example of its own, and behind the last one nothing is left.
+__device__ __forceinline__ void norm_write_sums(const NormBackward& p, int kind, int col, const float (&L)[NORM_PARTS]) {
+  const float sum = L[NORM_HEAD] + L[NORM_TOT], stat = norm_phi(p.phi, L[NORM_HEAD]) + L[NORM_STAT];
+  float *const out_sum = p.sums[2 * kind], *const out_stat = p.sums[2 * kind + 1];
+  if (out_sum) out_sum[col] = p.accumulate ? out_sum[col] + sum : sum;
+  if (out_stat) out_stat[col] = p.accumulate ? out_stat[col] + stat : stat;
+}
 
 // The rows that belong to examples.  Offsets that break the rules are cut to the tensor.
 __device__ __forceinline__ void norm_span(const NormBackward& p, long long& first, long long& last) {
@@ -834,11 +844,11 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     float s[SUMS];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
-    auto sums_of = [&](int k) {
+    auto sums_of = [&](int k, float mean_k, float rstd_k, float& wc, float& ws) {
       uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
       pairs(at_x, x, r0 + row0, k, fx);
       pairs(at_y, dy, r0 + row0, k, fy);
-      const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]);
+      const uint64_t m2 = f32x2_pack(-mean_k, -mean_k), r2 = f32x2_pack(rstd_k, rstd_k);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const uint64_t c = RMS ? fx[j] : f32x2_add(fx[j], m2);
@@ -852,58 +862,95 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       }
       float lo, hi;
       f32x2_unpack(s0, lo, hi);
-      s[k] = lo + hi;
-      if constexpr (!RMS) {
-        f32x2_unpack(s1, lo, hi);
-        s[R + k] = lo + hi;
-      }
+      wc = lo + hi;
+      f32x2_unpack(s1, lo, hi);
+      ws = lo + hi;
     };
     auto example_ends = [&] {
       // (opaque to the compiler, which would else compute the words' addresses before the loop and keep all of them)
       float* at = heads;
       int step = threads;
       asm volatile("" : "+l"(at), "+r"(step));
+      // (each test once, not once per feature)
+      auto all = [&](auto what) {
 #pragma unroll
-      for (int q = 0; q < KINDS; ++q)
+        for (int q = 0; q < KINDS; ++q)
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
+          for (int j = 0; j < P; ++j) {
+            what(q, j);
+            run[q][j] = 0ull;
+          }
+      };
+      if (!any_end) {
+        all([&](int q, int j) {
           float g[2];
           f32x2_unpack(run[q][j], g[0], g[1]);
-          if (!any_end) {
-            at[(q * NORM_COLS + 2 * j) * step] = g[0];
-            at[(q * NORM_COLS + 2 * j + 1) * step] = g[1];
-          } else if constexpr (SHORT) {
+          at[(q * NORM_COLS + 2 * j) * step] = g[0];
+          at[(q * NORM_COLS + 2 * j + 1) * step] = g[1];
+        });
+      } else if constexpr (SHORT) {
+        if (p.phi == 1) {
+          all([&](int q, int j) {
             tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
-            if (p.phi == 1) stat[q][j] = f32x2_fma(run[q][j], run[q][j], stat[q][j]);
-            else stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(p.phi, g[0]), norm_phi(p.phi, g[1])));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              at[(KEPT + q * NORM_COLS + 2 * j + e) * step] += g[e];
-              at[(2 * KEPT + q * NORM_COLS + 2 * j + e) * step] += norm_phi(p.phi, g[e]);
-            }
-          }
-          run[q][j] = 0ull;
+            stat[q][j] = f32x2_fma(run[q][j], run[q][j], stat[q][j]);
+          });
+        } else if (p.phi == 0) {
+          all([&](int q, int j) { tot[q][j] = f32x2_add(tot[q][j], run[q][j]); });      // (and stat is the same)
+        } else {
+          all([&](int q, int j) {
+            float g[2];
+            f32x2_unpack(run[q][j], g[0], g[1]);
+            tot[q][j] = f32x2_add(tot[q][j], run[q][j]);
+            stat[q][j] = f32x2_add(stat[q][j], f32x2_pack(norm_phi(2, g[0]), norm_phi(2, g[1])));
+          });
         }
+      } else {
+        all([&](int q, int j) {
+          float g[2];
+          f32x2_unpack(run[q][j], g[0], g[1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            at[(KEPT + q * NORM_COLS + 2 * j + e) * step] += g[e];
+            at[(2 * KEPT + q * NORM_COLS + 2 * j + e) * step] += norm_phi(p.phi, g[e]);
+          }
+        });
+      }
       any_end = true;
       end = ends.after(end);
       end_row = (int)min(end - r0, (long long)INT32_MAX) - 1;
     };
-    // R whole rows of one example, without a branch between them; otherwise row by row
+    // R whole rows of one example, without a branch between them; otherwise row by row, in a loop that stays one: an example's end is much code
     const bool full = row0 + R <= n_rows;
     if (full && end_row >= row0 + R - 1) {
       if (active) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) sums_of(k);
+        for (int k = 0; k < R; ++k) {
+          float ws;
+          sums_of(k, mu[k], rs[k], s[k], ws);
+          if constexpr (!RMS) s[R + k] = ws;
+        }
       }
       if (end_row == row0 + R - 1) example_ends();
     } else {
+      const int rows_left = min(R, n_rows - row0);
+#pragma unroll 1
+      for (int k = 0; k < rows_left; ++k) {
+        if (active) {
+          float mean_k = mu[0], rstd_k = rs[0], wc, ws;
 #pragma unroll
-      for (int k = 0; k < R; ++k)
-        if (row0 + k < n_rows) {
-          if (active) sums_of(k);
-          if (row0 + k == end_row) example_ends();
+          for (int q = 1; q < R; ++q) {
+            mean_k = k == q ? mu[q] : mean_k;
+            rstd_k = k == q ? rs[q] : rstd_k;
+          }
+          sums_of(k, mean_k, rstd_k, wc, ws);
+#pragma unroll
+          for (int q = 0; q < R; ++q) {
+            s[q] = k == q ? wc : s[q];
+            if constexpr (!RMS) s[R + q] = k == q ? ws : s[R + q];
+          }
         }
+        if (row0 + k == end_row) example_ends();
+      }
     }
     if constexpr (SUMMED) {
       norm_sums<SUMS>(s, G, group, t, slots, turn, NormAsIs{});
@@ -981,7 +1028,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       f32x2_unpack(run[k][j], g[0], g[1]);
       if constexpr (SHORT) {
         f32x2_unpack(tot[k][j], a[0], a[1]);
-        f32x2_unpack(stat[k][j], v[0], v[1]);
+        f32x2_unpack(p.phi == 0 ? tot[k][j] : stat[k][j], v[0], v[1]);
       } else {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -1013,6 +1060,10 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       const float Rr[NORM_PARTS] = {word(0, k, c, th), word(1, k, c, th), word(2, k, c, th), word(3, k, c, th)};
       norm_join(p.phi, le, L, re, Rr);
       le |= re;
+    }
+    if (MODE == NORM_WHOLE && blocks == 1) {      // nothing to join with
+      norm_write_sums(p, k, col, L);
+      continue;
     }
     float* out = p.parts + ((size_t)block * NORM_PARTS * KINDS + k) * d + col;
 #pragma unroll
@@ -1054,14 +1105,13 @@ norm_row_means_kernel(const T* __restrict__ x, const T* __restrict__ dy, const N
 constexpr int NORM_JOIN_WARPS = 32, NORM_JOIN_BATCH = 4;      // elements whose words a warp has in flight
 template <int KINDS>
 __global__ void __launch_bounds__(32 * NORM_JOIN_WARPS)
-norm_join_kernel(const float* __restrict__ parts, const int* __restrict__ ends, int blocks, int d, int phi, int accumulate,
-                 float* __restrict__ gain_sum, float* __restrict__ gain_stat, float* __restrict__ bias_sum, float* __restrict__ bias_stat) {
+norm_join_kernel(const NormBackward p, int blocks) {
   __shared__ float joined[NORM_JOIN_WARPS][NORM_PARTS][32];
   __shared__ int warp_end[NORM_JOIN_WARPS];
   sm100::griddep_launch_dependents();
   sm100::griddep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int units = (d + 31) / 32, kind = blockIdx.x / units, col = (blockIdx.x - kind * units) * 32 + lane;
+  const int d = p.d, phi = p.phi, units = (d + 31) / 32, kind = blockIdx.x / units, col = (blockIdx.x - kind * units) * 32 + lane;
   const int b0 = (int)((long long)blocks * warp / NORM_JOIN_WARPS), b1 = (int)((long long)blocks * (warp + 1) / NORM_JOIN_WARPS);
   float L[NORM_PARTS] = {0.f, 0.f, 0.f, 0.f};      // no rows: an element without an end
   bool le = false;
@@ -1071,8 +1121,8 @@ norm_join_kernel(const float* __restrict__ parts, const int* __restrict__ ends, 
 #pragma unroll
     for (int k = 0; k < NORM_JOIN_BATCH; ++k) {
       const bool live = b + k < b1;
-      const float* at = parts + ((size_t)(b + k) * NORM_PARTS * KINDS + kind) * d + col;
-      re[k] = live ? ends[b + k] : 0;
+      const float* at = p.parts + ((size_t)(b + k) * NORM_PARTS * KINDS + kind) * d + col;
+      re[k] = live ? p.ends[b + k] : 0;
 #pragma unroll
       for (int q = 0; q < NORM_PARTS; ++q) R[k][q] = live && col < d ? at[(size_t)q * KINDS * d] : 0.f;
     }
@@ -1093,11 +1143,7 @@ norm_join_kernel(const float* __restrict__ parts, const int* __restrict__ ends, 
     norm_join(phi, le, L, re, R);
     le |= re;
   }
-  // what came before the first end is an example of its own; behind the last end nothing is left
-  float sum = L[NORM_HEAD] + L[NORM_TOT], stat = norm_phi(phi, L[NORM_HEAD]) + L[NORM_STAT];
-  float *const out_sum = kind ? bias_sum : gain_sum, *const out_stat = kind ? bias_stat : gain_stat;
-  if (out_sum) out_sum[col] = accumulate ? out_sum[col] + sum : sum;
-  if (out_stat) out_stat[col] = accumulate ? out_stat[col] + stat : stat;
+  norm_write_sums(p, kind, col, L);
 }
 
 }  // namespace pe
