@@ -120,7 +120,7 @@ __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, 
 #pragma unroll
       for (int k = 0; k < N; ++k) slot[(first + (thread_in_group >> 5)) * N + k] = v[k];
     }
-    __syncthreads();
+    sm100::named_bar_sync(1 + group, G);      // (at most four groups of more than a warp)
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = 0.f;
     for (int w = 0; w < warps; ++w) {
@@ -163,7 +163,7 @@ __device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, i
     const int warps = G >> 5, first = group * warps;
     float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
     if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
-    __syncthreads();
+    sm100::named_bar_sync(1 + group, G);      // (at most four groups of more than a warp)
     // a lane sums the warps' values (l mod N / 2) 2 and the one after it, of every 64 / N-th warp
     float2 q = make_float2(0.f, 0.f);
     for (int w = lane / (N / 2); w < warps; w += 64 / N) {
