@@ -403,8 +403,9 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
  * G, out: bf16 [count, rows, cols], 16-byte aligned; out may be G.  count >= 0, rows, cols >= 1 (at most 2^30), count < 65536, count * rows * cols
  * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
  * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
- * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 per entry of A),
- * contents undefined afterwards.  Results repeat bit for bit.
+ * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 to 12 per entry of A, and up to 20 MB of partial products),
+ * contents undefined afterwards.  Results repeat bit for bit.  While the device status word is set (see pe_get_async_status) matrices whose
+ * sides are more than 64 and 128 are not written.
  */
 pe_status_t pe_orthogonalize(const void* G, int count, int rows, int cols, int steps, void* out, void* workspace,
                              size_t workspace_bytes, pe_stream_t stream);
@@ -421,7 +422,7 @@ size_t pe_orthogonalize_workspace_bytes(int count, int rows, int cols);
  * theta, m: fp32 [count, rows, cols], updated in place; sum_g: fp32, the out_mean of pe_linear_stats, s = grad_scale as for
  * microadam_step; theta_lp: optional bf16 copy of the new theta.  All 16-byte aligned, none overlapping another.  O(U) does not depend on U's scale;
  * update_scale is the caller's factor for it, often sqrt(max(1, rows / cols)).  Sizes, steps and workspace as for
- * pe_orthogonalize.  After PE_ERR_TIMEOUT theta is left as it was (of the matrices not yet written), m has been updated.
+ * pe_orthogonalize.  After PE_ERR_TIMEOUT theta is left as it was (of the tiles not yet written), m has been updated.
  */
 pe_status_t muon_step(float* theta, void* theta_lp, float* m, const float* sum_g, int count, int rows, int cols, int B,
                       float grad_scale, float lr, float beta, int nesterov, int steps, float update_scale, float weight_decay,
@@ -491,7 +492,7 @@ const char* pe_status_string(pe_status_t status);
  * NULL it receives a host int identifying the wait that expired (0 if none). */
 pe_status_t pe_get_async_status(pe_stream_t stream, int* detail);
 
-/* Cycle budget of every wait inside the tensor-core kernels on the CURRENT device (each wait of a thread
+/* Cycle budget of every wait inside the tensor-core kernels and the normalisation layers on the CURRENT device (each wait of a thread
  * on an on-chip barrier is bounded; a wait that exhausts the budget makes its kernel give up cleanly,
  * skip its outputs and latch PE_ERR_TIMEOUT for pe_get_async_status).  The default, restored by
  * cycles <= 0, is 2^32 cycles (about two seconds), far beyond any wait of a healthy launch; tests lower it

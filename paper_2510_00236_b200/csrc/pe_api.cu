@@ -2047,7 +2047,8 @@ pe_status_t pe_set_wait_limit_cycles(long long cycles) {
   if (rc != PE_OK) return rc;
   const long long v = cycles > 0 ? cycles : sm100::WAIT_CYCLE_LIMIT_DEFAULT;
   if (cudaMemcpyToSymbol(sm100::g_wait_cycle_limit, &v, sizeof v) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-  return ns_set_wait_limit(v);
+  const pe_status_t of_norms = norm_set_wait_limit(v);
+  return of_norms != PE_OK ? of_norms : ns_set_wait_limit(v);
 }
 
 int pe_set_fused_update(int mode) {

@@ -30,7 +30,9 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
 
 pe_status_t device_info(DeviceInfo** out);    // of the current device
 EncodeTiledFn encode_fn();
-pe_status_t ns_set_wait_limit(long long cycles);    // pe_set_wait_limit_cycles for the kernels of the orthogonalised update
+// pe_set_wait_limit_cycles for the kernels of the other translation units (each has its own copy of the limit)
+pe_status_t ns_set_wait_limit(long long cycles);
+pe_status_t norm_set_wait_limit(long long cycles);
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }

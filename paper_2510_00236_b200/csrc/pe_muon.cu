@@ -15,6 +15,7 @@ constexpr int NS_PAIRS = 74;            // pairs of SMs that launches and the wo
 struct NsPlan {
   int nt, splits;
   long long units;      // tiles of a matrix
+  double us;            // estimate
 };
 static long long ns_units(int rows, int cols, int nt, bool symmetric) {
   const long long tiles_m = (rows + 255) / 256, tiles_n = (cols + nt - 1) / nt;
@@ -27,7 +28,7 @@ static long long ns_units(int rows, int cols, int nt, bool symmetric) {
 // memory, write-out), and what joining slices costs.
 static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric) {
   const int stages = (k + NS_BK - 1) / NS_BK;
-  NsPlan best = {128, 1, 0};
+  NsPlan best = {128, 1, 0, 0.0};
   double best_us = 1e300;
   for (int nt : {64, 128, 256}) {
     const long long units = ns_units(rows, cols, nt, symmetric), tiles = units * count;
@@ -36,7 +37,7 @@ static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric)
       if (splits > 1 && tiles * splits > NS_PAIRS) break;
       const long long waves = (tiles * splits + NS_PAIRS - 1) / NS_PAIRS;
       const double us = waves * (((stages + splits - 1) / splits) * stage_us + fixed_us) + (splits > 1 ? 2.5 + 0.4 * splits : 0.0);
-      if (us < best_us) { best_us = us; best = {nt, splits, units}; }
+      if (us < best_us) { best_us = us; best = {nt, splits, units, us}; }
     }
   }
   return best;
@@ -44,10 +45,11 @@ static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric)
 
 struct NsLayout {
   NsPlan gram, poly, apply;        // A = X X^T, A A, Q X
+  bool pairs;                      // two steps at a time
   int n, m, ld_m, ld_n, tall;
   int partials;                    // partial sums of a matrix's norm
   int counters;                    // of split products, two words a tile
-  size_t norms, x[2], a, q, partial, counters_at, total; // byte offsets into the workspace
+  size_t norms, x[2], a, q, t, partial, counters_at, total; // byte offsets into the workspace
 };
 static bool ns_size_ok(int count, int rows, int cols) {
   return count >= 0 && rows >= 1 && cols >= 1 && rows <= (1 << 30) && cols <= (1 << 30) && (count == 0 || (long long)rows * cols <= ((1ll << 36) - 1) / count) && count <= 65535;
@@ -70,6 +72,13 @@ static NsLayout ns_layout(int count, int rows, int cols) {
   l.gram = plan_product(l.n, l.n, l.m, count, true);
   l.poly = plan_product(l.n, l.n, l.n, count, true);
   l.apply = plan_product(l.n, l.m, l.n, count, false);
+  // Two steps at a time where X is much longer than A: with Q = a I + b A + c A A, the next step's A is Q A Q and its polynomial another of A, so that X itself
+  // is multiplied once, by Q' Q, and not twice, and X X^T formed once: five products of n^3 for two more passes over X.  Not more steps than two: what rounding leaves in
+  // the directions of small singular values is multiplied by the square of the slope, up to 12 a step, in A, and by the slope, up to 3.4, in X; after two steps
+  // the errors of either way are those of fp32 products (2 to 6e-6), after three A is no longer positive and the iteration diverges.
+  // 8192 x 2048: 1057 us a call against 1526; 6 x 2048 x 512: 283 and 345; 512 x 32768: 496 and 706.  (Below 256 rows the launches are what counts, and there are more.)
+  l.pairs = l.n >= 256 && 3.0 * l.poly.us < 0.95 * (l.gram.us + l.apply.us);
+  l.t = part(l.pairs ? 4ull * count * l.n * l.ld_n : 0);
   size_t partial = 0;
   for (const NsPlan* p : {&l.gram, &l.poly, &l.apply})
     if (p->splits > 1) {
@@ -140,36 +149,55 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   double* norms = reinterpret_cast<double*>(ws + l.norms);
   __half* x[2] = {reinterpret_cast<__half*>(ws + l.x[0]), reinterpret_cast<__half*>(ws + l.x[1])};
   __half *const a = reinterpret_cast<__half*>(ws + l.a), *const q = reinterpret_cast<__half*>(ws + l.q);
-  pe_status_t rc = launch_dependent(ns_norms_kernel, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms,
+  const bool wide = (long long)rows * cols % 4 == 0 && (!s.given || (!s.bf16 && aligned(s.given, 16)));
+  pe_status_t rc = launch_dependent(wide ? ns_norms_kernel<true> : ns_norms_kernel<false>, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms,
                                     reinterpret_cast<unsigned int*>(ws + l.counters_at), l.counters);
   if (rc != PE_OK) return rc;
   const int tiles_m = (l.m + NS_INIT_TILE - 1) / NS_INIT_TILE, tiles_n = (l.n + NS_INIT_TILE - 1) / NS_INIT_TILE;
   rc = launch_dependent(ns_init_kernel, dim3((unsigned)(tiles_m * tiles_n), count), 256, 0, st, s, l.n, l.m, l.ld_m, l.tall, tiles_m, (const double*)norms,
                         l.partials, x[0], count);
   if (rc != PE_OK) return rc;
-  CUtensorMap xo[2], ao, qo, xa[2], xb_rows[2], xb_cols[2], aa, ab, qa;      // as A operand, as B operand row by row, as B operand with the contraction index slow
+  __half* const t = reinterpret_cast<__half*>(ws + l.t);
+  CUtensorMap xa[2], xb_rows[2], xb_cols[2], xo[2];      // as A operand, as B operand row by row, as B operand with the contraction index slow, as output
   for (int k = 0; k < 2; ++k)
     if (ns_map(&xa[k], x[k], 2 * count, l.n, l.m, l.ld_m, 128) != PE_OK || ns_map(&xb_rows[k], x[k], 2 * count, l.n, l.m, l.ld_m, l.gram.nt / 2) != PE_OK ||
         ns_map(&xb_cols[k], x[k], 2 * count, l.n, l.m, l.ld_m, NS_BK, l.apply.nt == 64) != PE_OK || ns_map(&xo[k], x[k], 2 * count, l.n, l.m, l.ld_m, 32, true) != PE_OK)
       return PE_ERR_CUDA;
-  if (ns_map(&aa, a, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ab, a, 2 * count, l.n, l.n, l.ld_n, l.poly.nt / 2) != PE_OK ||
-      ns_map(&qa, q, 2 * count, l.n, l.n, l.ld_n, 128) != PE_OK || ns_map(&ao, a, 2 * count, l.n, l.n, l.ld_n, 32, true) != PE_OK ||
-      ns_map(&qo, q, 2 * count, l.n, l.n, l.ld_n, 32, true) != PE_OK)
-    return PE_ERR_CUDA;
+  struct Square { CUtensorMap a, b, out; } A, Q, T;      // [n, n]
+  auto square = [&](Square& m, const __half* base) {
+    return ns_map(&m.a, base, 2 * count, l.n, l.n, l.ld_n, 128) == PE_OK && ns_map(&m.b, base, 2 * count, l.n, l.n, l.ld_n, l.poly.nt / 2) == PE_OK &&
+           ns_map(&m.out, base, 2 * count, l.n, l.n, l.ld_n, 32, true) == PE_OK;
+  };
+  if (!square(A, a) || !square(Q, q) || (l.pairs && !square(T, t))) return PE_ERR_CUDA;
   NsProduct p = out;
   p.count = count;
   p.dev_status = di->status_ptr;
   p.partial = reinterpret_cast<float*>(ws + l.partial);
   p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
-  for (int k = 0; k < steps; ++k) {
-    const int from = k & 1;
-    p.rows = p.cols = l.n; p.k = l.m; p.add = 0;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], ao, ao, p, st)) != PE_OK) return rc;
-    p.k = l.n; p.add = 1;
-    if ((rc = launch_planned<false, NS_SYMMETRIC>(l.poly, aa, ab, qo, ao, p, st)) != PE_OK) return rc;
-    p.cols = l.m; p.add = 0;
-    rc = k + 1 < steps ? launch_planned<true, NS_PLANES>(l.apply, qa, xb_cols[from], xo[from ^ 1], ao, p, st) : launch_planned<true, NS_FINAL>(l.apply, qa, xb_cols[from], xo[from ^ 1], ao, p, st);
-    if (rc != PE_OK) return rc;
+  p.rows = l.n;
+  auto gram = [&](int from) { p.cols = l.n; p.k = l.m; p.add = 0; return launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], A.out, A.out, p, st); };
+  // products of symmetric matrices that commute are symmetric; add: a I + b u + c u u
+  auto squares = [&](const Square& u, const Square& v, const Square& to, int add) {
+    p.cols = p.k = l.n; p.add = add;
+    return launch_planned<false, NS_SYMMETRIC>(l.poly, u.a, v.b, to.out, u.out, p, st);
+  };
+  auto apply = [&](const Square& u, int from, bool last) {
+    p.cols = l.m; p.k = l.n; p.add = 0;
+    return last ? launch_planned<true, NS_FINAL>(l.apply, u.a, xb_cols[from], xo[from ^ 1], A.out, p, st)
+                : launch_planned<true, NS_PLANES>(l.apply, u.a, xb_cols[from], xo[from ^ 1], A.out, p, st);
+  };
+  for (int left = steps, from = 0; left > 0; from ^= 1) {
+    if ((rc = gram(from)) != PE_OK || (rc = squares(A, A, Q, 1)) != PE_OK) return rc;
+    if (l.pairs && left >= 2) {
+      if ((rc = squares(Q, A, T, 0)) != PE_OK || (rc = squares(T, Q, A, 0)) != PE_OK ||      // A <- Q A Q
+          (rc = squares(A, A, T, 1)) != PE_OK || (rc = squares(T, Q, A, 0)) != PE_OK)        // T <- its polynomial, A <- T Q
+        return rc;
+      left -= 2;
+      if ((rc = apply(A, from, left == 0)) != PE_OK) return rc;
+    } else {
+      --left;
+      if ((rc = apply(Q, from, left == 0)) != PE_OK) return rc;
+    }
   }
   return PE_OK;
 }

@@ -51,6 +51,8 @@ __device__ __forceinline__ float ns_source_value(const NsSource& s, long long i)
 // Squared Frobenius norms, as gridDim.x partial sums per matrix (gridDim.y matrices), in 64 bits: no scale of the gradients overflows or vanishes.
 // Updates the momentum by the way, and zeroes the counters of split products.
 constexpr int NS_NORM_THREADS = 256;
+// WIDE: fp32, four elements to an access.
+template <bool WIDE>
 __global__ void __launch_bounds__(NS_NORM_THREADS)
 ns_norms_kernel(NsSource s, long long elems, double* __restrict__ partial, unsigned int* __restrict__ counters, int n_counters) {
   sm100::griddep_launch_dependents();
@@ -60,24 +62,56 @@ ns_norms_kernel(NsSource s, long long elems, double* __restrict__ partial, unsig
   __shared__ double warp_sum[NS_NORM_THREADS / 32];
   const long long base = (long long)blockIdx.y * elems, stride = (long long)gridDim.x * blockDim.x;
   double sum = 0.0;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < elems; i += 4 * stride) {
-    float v[4];
+  if constexpr (WIDE) {
+    const long long quads = elems / 4;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < quads; i += 2 * stride) {
+      float4 g[2], m[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const long long at = base + i + k * stride;
-      v[k] = 0.f;
-      if (i + k * stride < elems) {
-        if (s.given) {
-          v[k] = ns_source_value(s, at);
-        } else {
-          const float g = s.sum_g[at] * s.grad_scale, m = fmaf(s.beta, s.m[at], (1.f - s.beta) * g);
-          s.m[at] = m;
-          v[k] = s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * g) : m;
+      for (int k = 0; k < 2; ++k) {
+        const long long at = i + k * stride;
+        g[k] = m[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at < quads) {
+          g[k] = reinterpret_cast<const float4*>((s.given ? static_cast<const float*>(s.given) : s.sum_g) + base)[at];
+          if (!s.given) m[k] = reinterpret_cast<const float4*>(s.m + base)[at];
         }
       }
-    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum += (double)v[k] * (double)v[k];
+      for (int k = 0; k < 2; ++k) {
+        float v[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
+        if (!s.given) {
+          float mom[4] = {m[k].x, m[k].y, m[k].z, m[k].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float one = v[e] * s.grad_scale;
+            mom[e] = fmaf(s.beta, mom[e], (1.f - s.beta) * one);
+            v[e] = s.nesterov ? fmaf(s.beta, mom[e], (1.f - s.beta) * one) : mom[e];
+          }
+          if (i + k * stride < quads) reinterpret_cast<float4*>(s.m + base)[i + k * stride] = make_float4(mom[0], mom[1], mom[2], mom[3]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
+      }
+    }
+  } else {
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < elems; i += 4 * stride) {
+      float v[4];
+  #pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const long long at = base + i + k * stride;
+        v[k] = 0.f;
+        if (i + k * stride < elems) {
+          if (s.given) {
+            v[k] = ns_source_value(s, at);
+          } else {
+            const float g = s.sum_g[at] * s.grad_scale, m = fmaf(s.beta, s.m[at], (1.f - s.beta) * g);
+            s.m[at] = m;
+            v[k] = s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * g) : m;
+          }
+        }
+      }
+  #pragma unroll
+      for (int k = 0; k < 4; ++k) sum += (double)v[k] * (double)v[k];
+    }
   }
 #pragma unroll
   for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);

@@ -1,6 +1,5 @@
 // Entry points of the normalisation layers: argument checks, the choice of the launch, and the launches.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "pe_host.cuh"
@@ -60,8 +59,10 @@ template <typename T, int E, bool RMS>
 static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain, const float* bias, long long rows, int d, float eps, T* y,
                                   float* mean, float* rstd, cudaStream_t st) {
   const int wide = aligned(gain, 16) && aligned(bias, 16), ring_G = row_threads(d);
-  const long long ring_min = getenv("PE_RING") ? atoll(getenv("PE_RING")) : (1ll << 21);
-  if (ring_G <= NORM_MAX_THREADS && rows * d >= ring_min) {
+  // The ring where gain and bias out of L1 would hold rows up (16-bit rows of 1024 features or more: 256 x 1024 x 2048, 435 us against 563; 64 x 256 x 512, 11.4 and
+  // 11.2) or single features would (256 x 256 x 333, 49 and 128); fp32 rows go faster without (64 x 256 x 1024, 26.7 and 23.6), and so do few rows
+  // (8 x 256 x 1024, 7.0 and 5.8).
+  if (ring_G <= NORM_MAX_THREADS && rows * d >= (1ll << 22) && (E == 1 || (sizeof(T) == 2 && d >= 1024))) {
     const int groups = std::max(1, 256 / ring_G), threads = ring_G * groups, smem = (int)(groups * NORM_STAGES * (norm_slot_bytes(norm_rows<T>(), d, sizeof(T), true) + 8));
     const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 3072)));
     const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
@@ -258,6 +259,11 @@ static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, con
   const dim3 grid((unsigned)(kinds * ((d + 31) / 32)));
   return bias ? launch_dependent(norm_join_kernel<2>, grid, 32 * NORM_JOIN_WARPS, 0, st, a, p.blocks)
               : launch_dependent(norm_join_kernel<1>, grid, 32 * NORM_JOIN_WARPS, 0, st, a, p.blocks);
+}
+
+pe_status_t norm_set_wait_limit(long long cycles) {
+  if (cudaMemcpyToSymbol(sm100::g_wait_cycle_limit, &cycles, sizeof cycles) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  return PE_OK;
 }
 
 }  // namespace pe

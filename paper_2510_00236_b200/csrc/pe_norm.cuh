@@ -500,7 +500,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     norm_sums<R>(q, G, group, t, slots, turn, NormRstd{inv_d, eps});
     __syncwarp();
     if (t == 0) {
-      issue(b + S - 1);      // every thread of the group has left the slot before this one
+      if (waits) issue(b + S - 1);      // every thread of the group has left the slot before this one
 #pragma unroll
       for (int k = 0; k < R; ++k)
         if (row0 + k < n_rows) {
@@ -973,7 +973,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
     __syncwarp();
     // every thread of the group has left the slot before this one
-    if (t == 0) issue(b + S - 1);
+    if (t == 0 && waits) issue(b + S - 1);      // (a slot whose wait gave up is not filled again)
     auto write_row = [&](int k) {
       float k0 = 0.f, k1;
       if constexpr (SUMMED) {
