@@ -586,6 +586,8 @@ def pe_norm_forward(x, gain=None, bias=None, *, kind="layer", eps=1e-5, out=None
         op = out.data_ptr()
     else:
         op = _norm_input("out", out, shape, dtype, dev)
+        if op and op == xp:
+            raise ValueError("out must not overlap x")
     if rstd is None:
         rstd = x.new_empty(lead, dtype=torch.float32)
         rp = rstd.data_ptr()
