@@ -194,7 +194,7 @@ __device__ __forceinline__ void ns_small_rows(const float* a, const float* b, in
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = 0ull;
-#pragma unroll 2
+#pragma unroll 4
   for (int q = 0; q < k; q += 4) {
     ulonglong2 x[4], y[4];
 #pragma unroll
@@ -278,7 +278,7 @@ ns_small_kernel(NsSource s, NsResult o, int n, int m, int tall, int steps) {
       for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = 0ull;
       const bool in = c0 + 4 * tx < width;
       if (in) {
-#pragma unroll 2
+#pragma unroll 4
         for (int q = 0; q < NS_SMALL_N; q += 4) {
           float4 w[4];
           ulonglong2 x[4];
