@@ -155,15 +155,44 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
   return p;
 }
 
-// Clusters of `size` blocks of this kernel that the device runs at a time (0: not known yet); more would wait for a second round.
-static std::atomic<int> g_clusters[MAX_DEVICES][NORM_MAX_CLUSTER + 1];
-
 template <typename T, int E, bool RMS, int KINDS, int MODE, bool SHORT>
 static pe_status_t launch_rows(const T* x, const T* dy, T* dx, const NormBackward& a, const BackwardPlan& p, int smem, cudaStream_t st) {
   auto kernel = norm_backward_kernel<T, E, RMS, KINDS, MODE, SHORT>;
   static std::atomic<int> allowed[MAX_DEVICES];
   const pe_status_t rc = allow_smem(kernel, allowed, smem);
   return rc != PE_OK ? rc : launch_dependent(kernel, dim3(p.blocks, p.slabs), p.G * p.groups, smem, st, x, dy, dx, a);
+}
+template <typename T, int E, bool RMS, int KINDS, bool SHORT>
+static pe_status_t launch_cluster(const T* x, const T* dy, T* dx, NormBackward& a, BackwardPlan& p, int smem, cudaStream_t st) {
+  auto kernel = norm_backward_kernel<T, E, RMS, KINDS, NORM_CLUSTER, SHORT>;
+  static std::atomic<int> allowed[MAX_DEVICES];
+  const pe_status_t rc = allow_smem(kernel, allowed, smem);
+  if (rc != PE_OK) return rc;
+  a.cluster = p.slabs;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(p.G); cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.slabs; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  // clusters of this size that the device runs at a time (0: not asked yet); more would wait for a second round
+  static std::atomic<int> clusters[MAX_DEVICES][NORM_MAX_CLUSTER + 1];
+  int most = clusters[dev][p.slabs].load();
+  if (most == 0) {
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
+    if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) { cudaGetLastError(); return PE_ERR_CUDA; }
+    clusters[dev][p.slabs].store(most);
+  }
+  p.blocks = std::min(p.blocks, most);
+  cfg.numAttrs = 2;
+  cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
+  if (cudaLaunchKernelEx(&cfg, kernel, x, dy, dx, a) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
+  return check_launch();
 }
 template <typename T, int E, bool RMS, int KINDS>
 static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* dx, NormBackward& a, BackwardPlan& p, char* ws, cudaStream_t st) {
@@ -180,35 +209,8 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
   if (p.mode == NORM_WHOLE)
     return a.rows < 32ll * a.B || !p.kept ? launch_rows<T, E, RMS, KINDS, NORM_WHOLE, true>(x, dy, dx, a, p, smem, st)
                                           : launch_rows<T, E, RMS, KINDS, NORM_WHOLE, false>(x, dy, dx, a, p, smem, st);
-  if (p.mode == NORM_CLUSTER) {
-    auto kernel = norm_backward_kernel<T, E, RMS, KINDS, NORM_CLUSTER, false>;
-    static std::atomic<int> allowed[MAX_DEVICES];
-    const pe_status_t rc = allow_smem(kernel, allowed, smem);
-    if (rc != PE_OK) return rc;
-    a.cluster = p.slabs;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.slabs; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-    int most = g_clusters[dev][p.slabs].load();
-    if (most == 0) {
-      cfg.numAttrs = 1;
-      cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
-      if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) { cudaGetLastError(); return PE_ERR_CUDA; }
-      g_clusters[dev][p.slabs].store(most);
-    }
-    p.blocks = std::min(p.blocks, most);
-    cfg.numAttrs = 2;
-    cfg.gridDim = dim3((unsigned)(p.slabs * p.blocks));
-    if (cudaLaunchKernelEx(&cfg, kernel, x, dy, dx, a) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
-    return check_launch();
-  }
+  if (p.mode == NORM_CLUSTER)
+    return a.rows < 32ll * a.B ? launch_cluster<T, E, RMS, KINDS, true>(x, dy, dx, a, p, smem, st) : launch_cluster<T, E, RMS, KINDS, false>(x, dy, dx, a, p, smem, st);
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
                                           a, reinterpret_cast<float2*>(ws + p.means_at));
   if (rc != PE_OK) return rc;

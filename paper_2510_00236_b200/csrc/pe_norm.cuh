@@ -209,7 +209,7 @@ constexpr int NORM_COLS = 8;                     // features per thread
 constexpr int NORM_MAX_THREADS = 512;
 constexpr int NORM_STAGES = 3;
 template <typename T> __host__ __device__ constexpr int norm_rows() { return sizeof(T) == 2 ? 4 : 2; }      // R: a slot of 256 threads is 32 KB
-enum : int { NORM_WAIT_ROWS = 201 };
+enum : int { NORM_WAIT_ROWS = 201, NORM_WAIT_SUMS = 202 };
 
 // Bytes of a slot: R rows of one tensor and what alignment to 16 bytes adds at both ends (slab: of every row).
 __host__ __device__ constexpr size_t norm_slot_bytes(int R, int cols, int elem, bool whole) {
@@ -234,6 +234,11 @@ __device__ __forceinline__ uint32_t norm_fetch(uint32_t dst, uint8_t* dst_gen, c
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + (uint32_t)(lo - lo0)), "l"(lo),
                  "r"((uint32_t)(hi - lo)), "r"(bar) : "memory");
   return 0;
+}
+
+// The same where both ends are 16-byte aligned.
+__device__ __forceinline__ void norm_fetch_aligned(uint32_t dst, const void* src, uint32_t n, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(n), "r"(bar) : "memory");
 }
 
 // A thread's 8 features of a row in shared memory, as pairs: vector i is `offset[i]` bytes past byte `at`.  Vectors that are out of range have the offset of the
@@ -421,9 +426,14 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     const int n = min(R, n_rows - row), s = b % S;
     const T* src = x + (r0 + row) * d;
     const uint32_t bar = bars + 8 * s, dst = ring_s + (uint32_t)(s * slot);
-    const uint32_t bytes = norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, false);
-    mbar_arrive_expect_tx(bar, bytes);
-    norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, true);
+    if constexpr (E > 1) {
+      mbar_arrive_expect_tx(bar, (uint32_t)(n * d * (int)sizeof(T)));
+      norm_fetch_aligned(dst, src, (uint32_t)(n * d * (int)sizeof(T)), bar);
+    } else {
+      const uint32_t bytes = norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, false);
+      mbar_arrive_expect_tx(bar, bytes);
+      norm_fetch(dst, ring + s * slot, src, (size_t)n * d * sizeof(T), x, x + rows * d, bar, true);
+    }
   };
   if (t == 0)
     for (int b = 0; b < S - 1; ++b) issue(b);
@@ -699,7 +709,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   __shared__ __align__(16) float slots[2 * (NORM_MAX_THREADS / 32) * SUMS];
   __shared__ int group_end[256];
   __shared__ int abort_flag;
-  __shared__ float exchanged[MODE == NORM_CLUSTER ? 2 : 1][MODE == NORM_CLUSTER ? NORM_MAX_CLUSTER : 1][SUMS];
+  __shared__ __align__(16) float exchanged[MODE == NORM_CLUSTER ? 2 : 1][MODE == NORM_CLUSTER ? NORM_MAX_CLUSTER : 1][SUMS];      // the blocks' sums, of two turns
+  __shared__ uint64_t exchange_bar[2];
   const int G = p.G, d = p.d, group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G, threads = blockDim.x;
   const int rank = MODE == NORM_CLUSTER ? (int)cluster_ctarank() : 0, block = MODE == NORM_CLUSTER ? (int)blockIdx.x / p.cluster : (int)blockIdx.x;
   const int blocks = MODE == NORM_CLUSTER ? (int)gridDim.x / p.cluster : (int)gridDim.x;
@@ -708,7 +719,11 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   // [group][stage][x, dy], then a barrier per group and stage
   uint8_t* ring = smem + (size_t)group * S * 2 * slot;
   const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + (uint32_t)((size_t)groups * S * 2 * slot) + group * S * 8;
-  if (threadIdx.x == 0) abort_flag = 0;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    if (MODE == NORM_CLUSTER)
+      for (int k = 0; k < 2; ++k) mbar_init(smem_u32(&exchange_bar[k]), 1);
+  }
   if (t == 0) {
     for (int s = 0; s < S; ++s) mbar_init(bars + 8 * s, 1);
     fence_barrier_init();
@@ -724,31 +739,59 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const int n_rows = (int)(r1 - r0);
   if constexpr (MODE == NORM_CLUSTER) cluster_sync_all();      // every block of the cluster runs before one writes to it
   else __syncthreads();
-  // the group's first thread: rows r0 + b R .. into slot b % S
+  // Rows r0 + b R .. into slot b % S: by the group's first thread, or (slices of rows) by its first warp, a lane to a row.
   auto issue = [&](int b) {
     const long long row = r0 + (long long)b * R;
     if (row >= r1) return;
     const int n = (int)min((long long)R, r1 - row), s = b % S;
-    const uint32_t bar = bars + 8 * s;
-    const T *const x_end = x + p.rows * d, *const y_end = dy + p.rows * d;
-    const size_t at = (size_t)s * 2 * slot, row_slot = slot / R;
-    uint32_t bytes = 0;
-#pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
-      if constexpr (WHOLE) {
-        bytes += norm_fetch(ring_s + (uint32_t)at, ring + at, x + row * d, (size_t)n * d * sizeof(T), x, x_end, bar, pass == 1);
-        bytes += norm_fetch(ring_s + (uint32_t)(at + slot), ring + at + slot, dy + row * d, (size_t)n * d * sizeof(T), dy, y_end, bar, pass == 1);
+    const uint32_t bar = bars + 8 * s, at = (uint32_t)(s * 2 * slot);
+    if constexpr (WHOLE) {
+      if constexpr (E > 1) {
+        const uint32_t bytes = (uint32_t)(n * d * (int)sizeof(T));
+        mbar_arrive_expect_tx(bar, 2 * bytes);
+        norm_fetch_aligned(ring_s + at, x + row * d, bytes, bar);
+        norm_fetch_aligned(ring_s + at + (uint32_t)slot, dy + row * d, bytes, bar);
       } else {
-        for (int k = 0; k < n; ++k) {
-          const size_t ak = at + k * row_slot;
-          bytes += norm_fetch(ring_s + (uint32_t)ak, ring + ak, x + (row + k) * d + col0, (size_t)cols * sizeof(T), x, x_end, bar, pass == 1);
-          bytes += norm_fetch(ring_s + (uint32_t)(ak + slot), ring + ak + slot, dy + (row + k) * d + col0, (size_t)cols * sizeof(T), dy, y_end, bar, pass == 1);
+        const T *const x_end = x + p.rows * d, *const y_end = dy + p.rows * d;
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+          bytes += norm_fetch(ring_s + at, ring + at, x + row * d, (size_t)n * d * sizeof(T), x, x_end, bar, pass == 1);
+          bytes += norm_fetch(ring_s + at + (uint32_t)slot, ring + at + slot, dy + row * d, (size_t)n * d * sizeof(T), dy, y_end, bar, pass == 1);
+          if (pass == 0) mbar_arrive_expect_tx(bar, bytes);
         }
       }
-      if (pass == 0) mbar_arrive_expect_tx(bar, bytes);
+    } else {      // (one thread doing this for all rows kept the others waiting: 32 x 512 x 8192, 278 us and 206)
+      const uint32_t mine = at + t * (uint32_t)(slot / R);
+      const T *const xs = x + (row + t) * d + col0, *const ys = dy + (row + t) * d + col0;
+      if constexpr (E > 1) {
+        const uint32_t bytes = (uint32_t)(cols * (int)sizeof(T));
+        if (t == 0) mbar_arrive_expect_tx(bar, 2 * n * bytes);
+        __syncwarp();
+        if (t < n) {
+          norm_fetch_aligned(ring_s + mine, xs, bytes, bar);
+          norm_fetch_aligned(ring_s + mine + (uint32_t)slot, ys, bytes, bar);
+        }
+      } else {
+        const T *const x_end = x + p.rows * d, *const y_end = dy + p.rows * d;
+        const size_t size = (size_t)cols * sizeof(T);
+        uint32_t bytes = 0;
+        if (t < n) bytes = norm_fetch(ring_s + mine, ring + mine, xs, size, x, x_end, bar, false) +
+                           norm_fetch(ring_s + mine + (uint32_t)slot, ring + mine + slot, ys, size, dy, y_end, bar, false);
+#pragma unroll
+        for (int q = 1; q < R; q *= 2) bytes += __shfl_xor_sync(0xffffffffu, bytes, q);
+        __syncwarp();      // what lanes have copied themselves is there before the arrival
+        if (t == 0) mbar_arrive_expect_tx(bar, bytes);
+        __syncwarp();
+        if (t < n) {
+          norm_fetch(ring_s + mine, ring + mine, xs, size, x, x_end, bar, true);
+          norm_fetch(ring_s + mine + (uint32_t)slot, ring + mine + slot, ys, size, dy, y_end, bar, true);
+        }
+      }
     }
   };
-  if (t == 0)
+  const bool issues = WHOLE ? t == 0 : t < 32;
+  if (issues)
     for (int b = 0; b < S - 1; ++b) issue(b);
   uint64_t gain[P], run[KINDS][P], tot[SHORT ? KINDS : 1][SHORT ? P : 1], stat[SHORT ? KINDS : 1][SHORT ? P : 1];
   {
@@ -787,7 +830,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const uint32_t ring0 = (uint32_t)((size_t)group * S * 2 * slot) + (uint32_t)(t * E * sizeof(T));      // this thread's first vector of slot 0
   const uint32_t row_bytes = WHOLE ? (uint32_t)(d * sizeof(T)) : (uint32_t)(slot / R), out_bytes = (uint32_t)(d * sizeof(T));
   uint32_t at = ring0;
-  bool waits = true;
+  bool waits = true, exchange_waits = true;
   const float *mean_at = RMS ? nullptr : p.mean + r0, *rstd_at = p.rstd + r0;
   char* out = reinterpret_cast<char*>(dx + r0 * d + col0 + t * E);
   const bool strict = wait_cycle_limit() < WAIT_CYCLE_LIMIT_STRICT;
@@ -954,14 +997,20 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
     if constexpr (SUMMED) {
       norm_sums<SUMS>(s, G, group, t, slots, turn, NormAsIs{});
-      if constexpr (MODE == NORM_CLUSTER) {      // (a turn's words are written again two turns later, with a barrier of the cluster in between)
-        if ((int)threadIdx.x < p.cluster) {
-          const uint32_t to = map_to_cta(smem_u32(&exchanged[b & 1][rank][0]), threadIdx.x);
+      if constexpr (MODE == NORM_CLUSTER) {
+        // Every block sends its sums to all of them; a barrier of each counts what has arrived.  A block's words of a turn are written again two turns later, when it has
+        // read them: its own sums of the turn in between are only sent then, and everybody waits for those.  (A barrier of the cluster per turn instead:
+        // 32 x 512 x 8192, 299 us and 278.)
+        const uint32_t bar = smem_u32(&exchange_bar[b & 1]);
+        if (exchange_waits && threadIdx.x == 0) mbar_arrive_expect_tx(bar, (uint32_t)(p.cluster * SUMS * sizeof(float)));
+        if (exchange_waits && (int)threadIdx.x < p.cluster) {
+          const uint32_t to = map_to_cta(smem_u32(&exchanged[b & 1][rank][0]), threadIdx.x), to_bar = map_to_cta(bar, threadIdx.x);
 #pragma unroll
-          for (int k = 0; k < SUMS; ++k) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * k), "f"(s[k]) : "memory");
+          for (int k = 0; k < SUMS; k += 2)
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to + 4 * k), "f"(s[k]), "f"(s[k + 1]), "r"(to_bar) : "memory");
         }
+        if (exchange_waits) exchange_waits = mbar_wait_bounded(bar, (uint32_t)(b >> 1) & 1u, &abort_flag, p.dev_status, NORM_WAIT_SUMS, strict);
         __syncwarp();
-        cluster_sync_all();
 #pragma unroll
         for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
         for (int q = 0; q < p.cluster; ++q)
@@ -973,7 +1022,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
     __syncwarp();
     // every thread of the group has left the slot before this one
-    if (t == 0 && waits) issue(b + S - 1);      // (a slot whose wait gave up is not filled again)
+    if (issues && (WHOLE ? waits : __all_sync(0xffffffffu, waits))) issue(b + S - 1);      // (a slot whose wait gave up is not filled again)
     auto write_row = [&](int k) {
       float k0 = 0.f, k1;
       if constexpr (SUMMED) {
