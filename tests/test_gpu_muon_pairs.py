@@ -81,9 +81,10 @@ def test_waits_that_run_out_leave_parameters_alone():
     """The budget of every wait is lowered to a cycle: the kernels give up and say so; afterwards the same calls are right."""
     theta, m, sum_g = _noise(1, 512, 1024, 1)[0], _noise(1, 512, 1024, 2)[0], _noise(1, 512, 1024, 3)[0]
     start, m0 = theta.clone(), m.clone()
-    x = torch.randn(400, 16, 1024, device=DEV).to(torch.bfloat16)
+    # more rows than L2 holds: memory is slower than the kernels, so some of their many waits find nothing yet
+    x = torch.randn(64, 1024, 2048, device=DEV, dtype=torch.bfloat16)
     dy = torch.randn_like(x)
-    gain = torch.ones(1024, device=DEV)
+    gain = torch.ones(2048, device=DEV)
     y, mean, rstd = pe.pe_norm_forward(x, gain)
     want = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square")
     pe.pe_set_wait_limit_cycles(1, DEV)
