@@ -326,7 +326,8 @@ pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* 
  * four may be NULL to skip it (not all).  dx must not overlap x or dy.
  * workspace: device memory, 256-byte aligned, pe_norm_backward_workspace_bytes(B * T, d) bytes, contents undefined afterwards.
  * B == 0 or T == 0 leaves dx alone and writes zeros (accumulate: nothing).  The sums' order depends on the sizes and the device
- * alone: results repeat bit for bit.  An unknown kind or phi is PE_ERR_PHI.
+ * alone: results repeat bit for bit.  An unknown kind or phi is PE_ERR_PHI.  After PE_ERR_TIMEOUT (see pe_get_async_status) the outputs
+ * are invalid.
  */
 pe_status_t pe_norm_backward(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd, int B,
                              int T, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, void* dx, float* gain_sum,
@@ -339,7 +340,7 @@ pe_status_t pe_norm_backward_f32(const float* x, const float* dy, const float* g
                                  pe_stream_t stream);
 /* Same for a packed batch: x, dy, dx [total_rows, d], mean, rstd [total_rows], example b owns rows seq_offsets[b] ..
  * seq_offsets[b+1]-1 as for pe_linear_stats_ragged (device array, same rules; an empty sequence contributes phi(0) = 0).  Rows of dx
- * before the first and behind the last sequence are left as they were, and x and dy are not read there.
+ * before the first and behind the last sequence are left as they were, and what x, dy, mean and rstd hold there does not matter.
  * workspace: pe_norm_backward_workspace_bytes(total_rows, d) bytes. */
 pe_status_t pe_norm_backward_ragged(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd,
                                     const int* seq_offsets, int B, long long total_rows, int d, pe_norm_t kind, pe_phi_t phi,
@@ -401,7 +402,7 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
  * between 0.68 and 1.21, so that out is close to U V^T of G = U S V^T.  (The paper's statistics leave the mean gradient to elementwise updates; this
  * is the update for whole matrices beside them.)  G = 0 gives 0; an infinity or NaN gives NaN in that matrix alone.
  * G, out: bf16 [count, rows, cols], 16-byte aligned; out may be G.  count >= 0, rows, cols >= 1 (at most 2^30), count < 65536, count * rows * cols
- * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
+ * < 2^36 (and fewer than 2^30 tiles of 256 x 64), 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
  * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
  * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 to 12 per entry of A, and up to 20 MB of partial products),
  * contents undefined afterwards.  Results repeat bit for bit.  While the device status word is set (see pe_get_async_status) matrices whose

@@ -128,7 +128,6 @@ static pe_status_t launch_product(const CUtensorMap& a, const CUtensorMap& b, co
 }
 template <bool B_MN, int EPI>
 static pe_status_t launch_planned(const NsPlan& plan, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const CUtensorMap& add, NsProduct p, cudaStream_t st) {
-  if (2 * plan.units * p.count >= (1ll << 31)) return PE_ERR_DIM;      // (then a single slice)
   p.units = (int)plan.units;
   p.splits = plan.splits;
   if (plan.nt == 64) return launch_product<64, B_MN, EPI>(a, b, out, add, p, st);
@@ -205,7 +204,10 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
 static pe_status_t ns_check(int count, int rows, int cols, int steps, const void* workspace, size_t workspace_bytes) {
   if (!ns_size_ok(count, rows, cols) || steps < 1 || steps > NS_MAX_STEPS) return PE_ERR_DIM;
   if (count == 0) return PE_OK;
-  if (!workspace || workspace_bytes < ns_layout(count, rows, cols).total) return PE_ERR_WORKSPACE;
+  const NsLayout l = ns_layout(count, rows, cols);
+  for (const NsPlan* p : {&l.gram, &l.poly, &l.apply})      // blocks of a launch
+    if (2 * p->units * count >= (1ll << 31)) return PE_ERR_DIM;
+  if (!workspace || workspace_bytes < l.total) return PE_ERR_WORKSPACE;
   return aligned(workspace, 256) ? PE_OK : PE_ERR_ALIGN;
 }
 
