@@ -402,7 +402,7 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
  * between 0.68 and 1.21, so that out is close to U V^T of G = U S V^T.  (The paper's statistics leave the mean gradient to elementwise updates; this
  * is the update for whole matrices beside them.)  G = 0 gives 0; an infinity or NaN gives NaN in that matrix alone.
  * G, out: bf16 [count, rows, cols], 16-byte aligned; out may be G.  count >= 0, rows, cols >= 1 (at most 2^30), count < 65536, count * rows * cols
- * < 2^36 (and fewer than 2^30 tiles of 256 x 64), 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
+ * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
  * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
  * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 to 12 per entry of A, and up to 20 MB of partial products),
  * contents undefined afterwards.  Results repeat bit for bit.  While the device status word is set (see pe_get_async_status) matrices whose

@@ -1,15 +1,15 @@
-"""Sizes whose products would need more thread blocks than a launch has are refused before anything is enqueued."""
+"""The largest numbers of matrices and columns fit a launch: their sizes pass and the workspace is looked at next."""
 import ctypes
 
 import paper_2510_00236_b200 as pe
 from paper_2510_00236_b200 import build as pe_build
 
 
-def test_more_tiles_than_a_launch_has():
+def test_many_small_matrices_and_very_long_ones():
     pe_build.build_library()
     lib = pe.load_library()
     buf = ctypes.create_string_buffer(4096)
     p = (ctypes.addressof(buf) + 255) & ~255
-    # 65535 matrices of 1 x 1048577: 16385 tiles of 64 columns each, two blocks a tile
-    assert lib.pe_orthogonalize_f32(p, 65535, 1, 1048577, 5, p, p, 1 << 11, None) == 2
-    assert lib.pe_orthogonalize_f32(p, 65534, 1, 1048576, 5, p, p, 1 << 11, None) == 9       # fits: then the workspace is looked at
+    for count, rows, cols in ((65535, 1, 1048576), (1, 1 << 30, 1), (63, 1, 1 << 30), (1, 1 << 18, (1 << 18) - 1)):
+        assert lib.pe_orthogonalize_f32(p, count, rows, cols, 5, p, p, 1 << 11, None) == 9      # PE_ERR_WORKSPACE
+    assert lib.pe_orthogonalize_f32(p, 64, 1, 1 << 30, 5, p, p, 1 << 11, None) == 2              # PE_ERR_DIM
