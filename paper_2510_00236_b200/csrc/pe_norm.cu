@@ -64,7 +64,7 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
   // (8 x 256 x 1024, 7.0 and 5.8).
   if (ring_G <= NORM_MAX_THREADS && rows * d >= (1ll << 22) && (E == 1 || (sizeof(T) == 2 && d >= 1024))) {
     const int groups = std::max(1, 256 / ring_G), threads = ring_G * groups, smem = (int)(groups * NORM_STAGES * (norm_slot_bytes(norm_rows<T>(), d, sizeof(T), true) + 8));
-    const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 3072)));
+    const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 4096)));
     const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
     auto kernel = norm_forward_ring_kernel<T, E, RMS>;
     static std::atomic<int> allowed[MAX_DEVICES];
