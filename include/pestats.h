@@ -306,7 +306,8 @@ pe_status_t pe_token_sqstats_static(const void* X, const void* dY, int B, int T,
  * transformer normalises before every block.)
  * x, y: bf16 [rows, d], 16-byte aligned, not overlapping; gain, bias: fp32 [d], 4-byte aligned, NULL for ones / zeros; mean, rstd: fp32 [rows], 4-byte
  * aligned, what pe_norm_backward reads; NULL to skip (PE_NORM_RMS writes no mean).  rows >= 0, d >= 1, rows * d < 2^40, eps >= 0.
- * Sums are fp32: the mean first, then the squared deviations from it.  y is rounded once.  An unknown kind is PE_ERR_PHI.
+ * Sums are fp32: the mean first, then the squared deviations from it.  y is rounded once.  An unknown kind is PE_ERR_PHI.  After PE_ERR_TIMEOUT (see
+ * pe_get_async_status) some rows of y, mean and rstd are as they were before.
  */
 typedef enum { PE_NORM_LAYER = 0, PE_NORM_RMS = 1 } pe_norm_t;
 pe_status_t pe_norm_forward(const void* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind,
@@ -326,8 +327,8 @@ pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* 
  * four may be NULL to skip it (not all).  dx must not overlap x or dy.
  * workspace: device memory, 256-byte aligned, pe_norm_backward_workspace_bytes(B * T, d) bytes, contents undefined afterwards.
  * B == 0 or T == 0 leaves dx alone and writes zeros (accumulate: nothing).  The sums' order depends on the sizes and the device
- * alone: results repeat bit for bit.  An unknown kind or phi is PE_ERR_PHI.  After PE_ERR_TIMEOUT (see pe_get_async_status) the outputs
- * are invalid.
+ * alone: results repeat bit for bit.  An unknown kind or phi is PE_ERR_PHI.  After PE_ERR_TIMEOUT (see pe_get_async_status) some rows of dx
+ * and all four sums are as they were before (accumulate: nothing has been added).
  */
 pe_status_t pe_norm_backward(const void* x, const void* dy, const float* gain, const float* mean, const float* rstd, int B,
                              int T, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, void* dx, float* gain_sum,

@@ -149,7 +149,7 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
   const long long most = p.mode == NORM_WHOLE ? sm_count * std::max(1, 512 / (p.G * p.groups)) : std::max(1, (p.mode == NORM_SLAB ? 2 : 1) * sm_count / p.slabs);
   p.blocks = (int)std::min(want, most);
   p.ends_at = align_up((size_t)p.blocks * NORM_PARTS * kinds * d * sizeof(float), 256);
-  p.heads_at = p.ends_at + align_up((size_t)p.blocks * sizeof(int), 256);
+  p.heads_at = p.ends_at + align_up((size_t)p.blocks * (p.mode == NORM_CLUSTER ? p.slabs : 1) * sizeof(int), 256);
   p.means_at = p.heads_at + align_up((size_t)p.blocks * p.slabs * (p.kept ? 3 : 1) * kinds * NORM_COLS * p.G * p.groups * sizeof(float), 256);
   p.bytes = p.means_at + (p.mode == NORM_SLAB ? align_up((size_t)rows * sizeof(float2), 256) : 0);
   return p;
@@ -212,7 +212,7 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
   if (p.mode == NORM_CLUSTER)
     return a.rows < 32ll * a.B ? launch_cluster<T, E, RMS, KINDS, true>(x, dy, dx, a, p, smem, st) : launch_cluster<T, E, RMS, KINDS, false>(x, dy, dx, a, p, smem, st);
   const pe_status_t rc = launch_dependent(norm_row_means_kernel<T, RMS>, dim3((unsigned)std::min<long long>(a.rows, 2ll * di->sm_count)), 1024, 0, st, x, dy,
-                                          a, reinterpret_cast<float2*>(ws + p.means_at));
+                                          a, reinterpret_cast<float2*>(ws + p.means_at), p.blocks);
   if (rc != PE_OK) return rc;
   return launch_rows<T, E, RMS, KINDS, NORM_SLAB, true>(x, dy, dx, a, p, smem, st);
 }

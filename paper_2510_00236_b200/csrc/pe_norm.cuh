@@ -509,11 +509,12 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     }
     norm_sums<R>(q, G, group, t, slots, turn, NormRstd{inv_d, eps});
     __syncwarp();
+    const bool lost = *(volatile int*)&abort_flag != 0;      // a thread of the group (or block) has given up: these sums, or later ones, are of rows that are not there
     if (t == 0) {
       if (waits) issue(b + S - 1);      // every thread of the group has left the slot before this one
 #pragma unroll
       for (int k = 0; k < R; ++k)
-        if (row0 + k < n_rows) {
+        if (row0 + k < n_rows && !lost) {
           if (!RMS && mean) mean[r0 + row0 + k] = mu[k];
           if (rstd) rstd[r0 + row0 + k] = q[k];
         }
@@ -532,7 +533,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
       for (int i = 0; i < NV; ++i)
         if (E == 8 || (i * G + t) * E < d) NormVec<T, E>::store(reinterpret_cast<T*>(out + (k * row_bytes + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)))), o[i]);
     };
-    if (active) {
+    if (active && !lost) {
       if (row0 + R <= n_rows) {
 #pragma unroll
         for (int k = 0; k < R; ++k) write_row(k);
@@ -601,6 +602,7 @@ norm_forward_wide_kernel(const T* __restrict__ x, const float* __restrict__ gain
 // (L without an end, R): head = L.head + R.head, the rest R's.  (L with an end, R without): tail = L.tail + R.head.  Both with:
 // the example L.tail + R.head is complete and goes into tot.  No atomics: the sums' order is fixed by the launch's shape.
 enum : int { NORM_HEAD = 0, NORM_TOT = 1, NORM_STAT = 2, NORM_TAIL = 3, NORM_PARTS = 4 };
+enum : int { NORM_END = 1, NORM_LOST = 2 };
 __device__ __forceinline__ float norm_phi(int phi, float g) {
   return phi == 1 ? g * g : phi == 2 ? (float)((g > 0.f) - (g < 0.f)) : g;
 }
@@ -631,7 +633,7 @@ struct NormBackward {
   int accumulate;
   int cluster;                          // NORM_CLUSTER: blocks of a cluster
   float* parts;                         // [blocks][NORM_PARTS][kinds][d]; a block's element
-  int* ends;                            // [blocks]: whether an example ends in the block's rows
+  int* ends;                            // [blocks][blocks of a cluster]: NORM_END where an example ends in the block's rows, NORM_LOST where a wait gave up
   float* heads;                         // what the blocks' threads keep here until their rows are done (see there)
   unsigned int* dev_status;
   const float2* row_means;              // of each row: (mean(w xh), mean(w)), where a kernel before this one found them
@@ -995,15 +997,18 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
         if (row0 + k == end_row) example_ends();
       }
     }
+    bool lost;      // a thread of the group (or block) has given up: these sums, or later ones, are of rows that are not there
     if constexpr (SUMMED) {
       norm_sums<SUMS>(s, G, group, t, slots, turn, NormAsIs{});
+      __syncwarp();
+      lost = *(volatile int*)&abort_flag != 0;
       if constexpr (MODE == NORM_CLUSTER) {
         // Every block sends its sums to all of them; a barrier of each counts what has arrived.  A block's words of a turn are written again two turns later, when it has
         // read them: its own sums of the turn in between are only sent then, and everybody waits for those.  (A barrier of the cluster per turn instead:
         // 32 x 512 x 8192, 299 us and 278.)
         const uint32_t bar = smem_u32(&exchange_bar[b & 1]);
         if (exchange_waits && threadIdx.x == 0) mbar_arrive_expect_tx(bar, (uint32_t)(p.cluster * SUMS * sizeof(float)));
-        if (exchange_waits && (int)threadIdx.x < p.cluster) {
+        if (exchange_waits && !lost && (int)threadIdx.x < p.cluster) {      // (sums of rows that are not there are not sent: the others' waits for them run out)
           const uint32_t to = map_to_cta(smem_u32(&exchanged[b & 1][rank][0]), threadIdx.x), to_bar = map_to_cta(bar, threadIdx.x);
 #pragma unroll
           for (int k = 0; k < SUMS; k += 2)
@@ -1019,6 +1024,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       }
     } else {
       __syncthreads();
+      lost = *(volatile int*)&abort_flag != 0;
     }
     __syncwarp();
     // every thread of the group has left the slot before this one
@@ -1047,7 +1053,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       for (int i = 0; i < NV; ++i)
         if (E == 8 || (i * G + t) * E < cols) NormVec<T, E>::store(reinterpret_cast<T*>(out + (k * out_bytes + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)))), o[i]);
     };
-    if (dx && active) {
+    if (dx && active && !lost && exchange_waits) {
       if (full) {
 #pragma unroll
         for (int k = 0; k < R; ++k) write_row(k);
@@ -1111,17 +1117,18 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
       le |= re;
     }
     if (MODE == NORM_WHOLE && blocks == 1) {      // nothing to join with
-      norm_write_sums(p, k, col, L);
+      if (!abort_flag) norm_write_sums(p, k, col, L);
       continue;
     }
     float* out = p.parts + ((size_t)block * NORM_PARTS * KINDS + k) * d + col;
 #pragma unroll
     for (int q = 0; q < NORM_PARTS; ++q) out[(size_t)q * KINDS * d] = L[q];
   }
-  if (threadIdx.x == 0 && rank == 0 && blockIdx.y == 0) {
-    int l_end = 0;
-    for (int g = 0; g < groups; ++g) l_end |= group_end[g];
-    p.ends[block] = l_end;
+  if (threadIdx.x == 0) {
+    int found = abort_flag ? NORM_LOST : 0;
+    for (int g = 0; g < groups; ++g) found |= group_end[g] ? NORM_END : 0;
+    if (MODE == NORM_SLAB) atomicOr(p.ends + block, found);      // (zeroed by norm_row_means_kernel)
+    else p.ends[MODE == NORM_CLUSTER ? block * p.cluster + rank : block] = found;
   }
   if constexpr (MODE == NORM_CLUSTER) cluster_sync_all();      // nobody leaves while its shared memory may be written
 }
@@ -1129,10 +1136,12 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
 // The two means of every row, for rows wider than a block of norm_backward_kernel: a block per row.
 template <typename T, bool RMS>
 __global__ void __launch_bounds__(1024)
-norm_row_means_kernel(const T* __restrict__ x, const T* __restrict__ dy, const NormBackward p, float2* __restrict__ row_means) {
+norm_row_means_kernel(const T* __restrict__ x, const T* __restrict__ dy, const NormBackward p, float2* __restrict__ row_means, int blocks) {
   __shared__ float slots[2 * NORM_MAX_WARPS * 2];
   sm100::griddep_launch_dependents();
   sm100::griddep_wait();
+  if (blockIdx.x == 0)
+    for (int b = threadIdx.x; b < blocks; b += blockDim.x) p.ends[b] = 0;
   long long first, last;
   norm_span(p, first, last);
   const float inv_d = 1.f / (float)p.d;
@@ -1150,7 +1159,8 @@ norm_row_means_kernel(const T* __restrict__ x, const T* __restrict__ dy, const N
   }
 }
 
-// Joins the blocks' elements, in their order: a block per 32 features, its warps take consecutive elements and are joined in turn.
+// Joins the blocks' elements, in their order: a block per 32 features, its warps take consecutive elements and are joined in turn.  Where a wait gave up in any of
+// them all sums are left as they were.
 constexpr int NORM_JOIN_WARPS = 32, NORM_JOIN_BATCH = 4;      // elements whose words a warp has in flight
 template <int KINDS>
 __global__ void __launch_bounds__(32 * NORM_JOIN_WARPS)
@@ -1164,6 +1174,9 @@ norm_join_kernel(const NormBackward p, int blocks) {
   const int b0 = (int)((long long)blocks * warp / NORM_JOIN_WARPS), b1 = (int)((long long)blocks * (warp + 1) / NORM_JOIN_WARPS);
   float L[NORM_PARTS] = {0.f, 0.f, 0.f, 0.f};      // no rows: an element without an end
   bool le = false;
+  const int ranks = p.cluster > 0 ? p.cluster : 1;
+  int lost = 0;
+  for (int i = threadIdx.x; i < blocks * ranks; i += blockDim.x) lost |= p.ends[i] & NORM_LOST;
   for (int b = b0; b < b1; b += NORM_JOIN_BATCH) {
     float R[NORM_JOIN_BATCH][NORM_PARTS];
     int re[NORM_JOIN_BATCH];
@@ -1171,7 +1184,7 @@ norm_join_kernel(const NormBackward p, int blocks) {
     for (int k = 0; k < NORM_JOIN_BATCH; ++k) {
       const bool live = b + k < b1;
       const float* at = p.parts + ((size_t)(b + k) * NORM_PARTS * KINDS + kind) * d + col;
-      re[k] = live ? p.ends[b + k] : 0;
+      re[k] = live ? p.ends[(b + k) * ranks] & NORM_END : 0;
 #pragma unroll
       for (int q = 0; q < NORM_PARTS; ++q) R[k][q] = live && col < d ? at[(size_t)q * KINDS * d] : 0.f;
     }
@@ -1184,8 +1197,7 @@ norm_join_kernel(const NormBackward p, int blocks) {
 #pragma unroll
   for (int q = 0; q < NORM_PARTS; ++q) joined[warp][q][lane] = L[q];
   if (lane == 0) warp_end[warp] = le;
-  __syncthreads();
-  if (warp != 0 || col >= d) return;
+  if (__syncthreads_or(lost) || warp != 0 || col >= d) return;
   for (int w = 1; w < NORM_JOIN_WARPS; ++w) {
     const bool re = warp_end[w] != 0;
     const float R[NORM_PARTS] = {joined[w][0][lane], joined[w][1][lane], joined[w][2][lane], joined[w][3][lane]};

@@ -67,3 +67,53 @@ def test_waits_that_run_out_are_reported_and_the_library_stays_usable(short_wait
     th_ref, _, _ = oracle.microadam_step(W0, np.zeros_like(W0), np.zeros_like(W0), st.sum_g, st.sum_g2, B, lr=1e-3, beta1=0.9, beta2=0.999,
                                          eps=1e-8, step=1)
     assert np.linalg.norm((th.cpu().numpy() - W0) - (th_ref - W0)) <= FROB_TOL * np.linalg.norm(th_ref - W0)
+
+
+# whole rows through the forward ring, aligned and of an odd width; slices in clusters; rows wider than that; a single block
+NORM_ROWS = [(64, 1024, 2048, torch.bfloat16), (64, 512, 1001, torch.float32), (16, 512, 8192, torch.bfloat16), (8, 128, 40000, torch.bfloat16), (1, 40, 64, torch.float32),
+             (64, 2048, 40, torch.bfloat16)]
+
+
+def _norm_rows(B, T, d, dtype):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(d)
+    x, dy = (torch.randn(B, T, d, generator=g, device=DEV).to(dtype) for _ in range(2))
+    return x, dy, 1 + 0.1 * torch.randn(d, generator=g, device=DEV)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("B,T,d,dtype", NORM_ROWS)
+def test_normalisation_layers_whose_waits_run_out_write_nothing_wrong(B, T, d, dtype, kind):
+    """Every value is either right or as it was; the sums, all of them or none; and the same calls are right afterwards."""
+    x, dy, gain = _norm_rows(B, T, d, dtype)
+    y, mean, rstd = pe.pe_norm_forward(x, gain, kind=kind)
+    sums = dict(zip(("gain_sum", "gain_stat", "bias_sum", "bias_stat"), torch.arange(4 * d, device=DEV, dtype=torch.float32).view(4, d).unbind()))
+    full = {k: v.clone() for k, v in sums.items()}
+    dx = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind, accumulate=True, **full)[0]
+    assert pe.pe_get_async_status(DEV) == (0, 0)
+    ran_out = 0
+    for _ in range(4):
+        got_y, got_r, got_dx = torch.full_like(x, -77.0), torch.full_like(rstd, -77.0), torch.full_like(x, -77.0)
+        got_m = None if mean is None else torch.full_like(mean, -77.0)
+        got = {k: v.clone() for k, v in sums.items()}
+        pe.pe_set_wait_limit_cycles(1, DEV)
+        try:
+            pe.pe_norm_forward(x, gain, kind=kind, out=got_y, mean=got_m, rstd=got_r)
+            forward = pe.pe_get_async_status(DEV)
+            pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind, accumulate=True, dx=got_dx, **got)
+            backward = pe.pe_get_async_status(DEV)
+        finally:
+            pe.pe_set_wait_limit_cycles(0, DEV)
+        assert forward[0] in (0, PE_ERR_TIMEOUT) and backward[0] in (0, PE_ERR_TIMEOUT)
+        for have, want, status in ((got_y, y, forward), (got_r, rstd, forward), (got_m, mean, forward), (got_dx, dx, backward)):
+            if have is not None:
+                assert torch.all((have == want) | ((have == -77.0) & (status[0] != 0)))
+        for k in sums:
+            assert torch.equal(got[k], sums[k] if backward[0] else full[k]), k
+        ran_out += backward[0] != 0
+    if (B, T, d) == (64, 1024, 2048):
+        assert ran_out      # (memory is slower than the kernel)
+    again = {k: v.clone() for k, v in sums.items()}
+    assert torch.equal(pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind, accumulate=True, **again)[0], dx)
+    assert all(torch.equal(again[k], full[k]) for k in sums) and torch.equal(pe.pe_norm_forward(x, gain, kind=kind)[0], y)
+    assert pe.pe_get_async_status(DEV) == (0, 0)
