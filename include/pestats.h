@@ -406,8 +406,8 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
  * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
  * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
  * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 to 12 per entry of A, and up to 20 MB of partial products),
- * contents undefined afterwards.  Results repeat bit for bit.  While the device status word is set (see pe_get_async_status) matrices whose
- * sides are more than 64 and 128 are not written.
+ * contents undefined afterwards.  Results repeat bit for bit.  After PE_ERR_TIMEOUT (see pe_get_async_status) out is as it was, but for tiles of the last
+ * product that were written before its own wait ran out.
  */
 pe_status_t pe_orthogonalize(const void* G, int count, int rows, int cols, int steps, void* out, void* workspace,
                              size_t workspace_bytes, pe_stream_t stream);

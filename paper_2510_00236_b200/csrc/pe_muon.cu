@@ -48,7 +48,7 @@ struct NsLayout {
   bool pairs;                      // two steps at a time
   int n, m, ld_m, ld_n, tall;
   int partials;                    // partial sums of a matrix's norm
-  int counters;                    // of split products, two words a tile
+  int counters;                    // of split products, two words a tile; a word for products that gave up is behind them
   size_t norms, x[2], a, q, t, partial, counters_at, total; // byte offsets into the workspace
 };
 static bool ns_size_ok(int count, int rows, int cols) {
@@ -86,7 +86,7 @@ static NsLayout ns_layout(int count, int rows, int cols) {
       l.counters = std::max(l.counters, (int)(2 * p->units * count));
     }
   l.partial = part(partial);
-  l.counters_at = part((size_t)l.counters * sizeof(unsigned int));
+  l.counters_at = part(((size_t)l.counters + 1) * sizeof(unsigned int));
   l.total = at;
   return l;
 }
@@ -150,7 +150,7 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   __half *const a = reinterpret_cast<__half*>(ws + l.a), *const q = reinterpret_cast<__half*>(ws + l.q);
   const bool wide = (long long)rows * cols % 4 == 0 && (!s.given || (!s.bf16 && aligned(s.given, 16)));
   pe_status_t rc = launch_dependent(wide ? ns_norms_kernel<true> : ns_norms_kernel<false>, dim3(l.partials, count), NS_NORM_THREADS, 0, st, s, (long long)rows * cols, norms,
-                                    reinterpret_cast<unsigned int*>(ws + l.counters_at), l.counters);
+                                    reinterpret_cast<unsigned int*>(ws + l.counters_at), l.counters + 1);
   if (rc != PE_OK) return rc;
   const int tiles_m = (l.m + NS_INIT_TILE - 1) / NS_INIT_TILE, tiles_n = (l.n + NS_INIT_TILE - 1) / NS_INIT_TILE;
   rc = launch_dependent(ns_init_kernel, dim3((unsigned)(tiles_m * tiles_n), count), 256, 0, st, s, l.n, l.m, l.ld_m, l.tall, tiles_m, (const double*)norms,
@@ -173,6 +173,7 @@ static pe_status_t newton_schulz(DeviceInfo* di, const NsSource& s, int count, i
   p.dev_status = di->status_ptr;
   p.partial = reinterpret_cast<float*>(ws + l.partial);
   p.counters = reinterpret_cast<unsigned int*>(ws + l.counters_at);
+  p.gave_up = p.counters + l.counters;
   p.rows = l.n;
   auto gram = [&](int from) { p.cols = l.n; p.k = l.m; p.add = 0; return launch_planned<false, NS_SYMMETRIC>(l.gram, xa[from], xb_rows[from], A.out, A.out, p, st); };
   // products of symmetric matrices that commute are symmetric; add: a I + b u + c u u

@@ -49,7 +49,7 @@ __device__ __forceinline__ float ns_source_value(const NsSource& s, long long i)
   return s.nesterov ? fmaf(s.beta, m, (1.f - s.beta) * (s.sum_g[i] * s.grad_scale)) : m;
 }
 // Squared Frobenius norms, as gridDim.x partial sums per matrix (gridDim.y matrices), in 64 bits: no scale of the gradients overflows or vanishes.
-// Updates the momentum by the way, and zeroes the counters of split products.
+// Updates the momentum by the way, and zeroes the counters of split products and the word behind them, which says whether a product gave up.
 constexpr int NS_NORM_THREADS = 256;
 // WIDE: fp32, four elements to an access.
 template <bool WIDE>
@@ -338,6 +338,7 @@ struct NsProduct {
   int splits;                    // slices of the contraction index, each a pair's; the last one done adds the partial tiles up in their order
   float* partial;                // [splits][units * count][2][8 warps][NT / 2][32], where there are several
   unsigned int* counters;        // [units * count][2], zero before and after a product
+  unsigned int* gave_up;         // set where a wait of this call's products ran out: the last one then writes nothing
   int add;                       // NS_SYMMETRIC: 0, or 1: the result is a I + b A + c (product), A by map_add
   // NS_FINAL: the result itself, [rows, cols] per matrix, or transposed: [cols, rows]
   int transposed;
@@ -596,6 +597,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       float* at = p.partial + (slice * tiles * 16 + mine) * (COLS * 32) + lane;
 #pragma unroll
       for (int j = 0; j < COLS; ++j) __stcg(at + j * 32, acc[j]);
+      if (!ok && lane == 0) *reinterpret_cast<volatile unsigned int*>(p.gave_up) = 1u;      // (before this slice counts as done)
       __threadfence();
       named_bar_sync(1, 256);
       if (threadIdx.x == 64) {
@@ -617,7 +619,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
       }
     }
-    if (EPI == NS_FINAL && *reinterpret_cast<volatile unsigned int*>(p.dev_status) != 0u) write = false;      // an earlier product may have given up
+    if (EPI == NS_FINAL && *reinterpret_cast<volatile unsigned int*>(p.gave_up) != 0u) write = false;      // (an earlier product, or a slice of this tile)
     if (ok && write) {
       // A warp's 32 x 32 pieces; lanes hold rows.
       if constexpr (EPI == NS_SYMMETRIC && COLS > 32) {
@@ -737,6 +739,7 @@ ns_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {      // a wait gave up: loads in flight may still land here, so the block stays a while
+    if (threadIdx.x == 0) *reinterpret_cast<volatile unsigned int*>(p.gave_up) = 1u;
     const long long t0 = clock64();
     while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
   }

@@ -117,3 +117,28 @@ def test_normalisation_layers_whose_waits_run_out_write_nothing_wrong(B, T, d, d
     assert torch.equal(pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind, accumulate=True, **again)[0], dx)
     assert all(torch.equal(again[k], full[k]) for k in sums) and torch.equal(pe.pe_norm_forward(x, gain, kind=kind)[0], y)
     assert pe.pe_get_async_status(DEV) == (0, 0)
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 40, 72), (1, 300, 500), (2, 320, 4000)])
+def test_a_status_of_an_earlier_call_does_not_stop_the_orthogonalised_update(count, rows, cols):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows)
+    G, theta0 = (torch.randn(count, rows, cols, generator=g, device=DEV) for _ in range(2))
+    want = pe.pe_orthogonalize(G)
+    stepped, moved = theta0.clone(), torch.zeros_like(G)
+    pe.muon_step(stepped, moved, G, 4, lr=0.1, beta=0.9)
+    assert pe.pe_get_async_status(DEV) == (0, 0)
+    li = inputs.gaussian_layer(8, 512, 256, 512, seed=31, device=DEV)
+    pe.pe_set_path(pe.PATH_TENSOR)
+    pe.pe_set_wait_limit_cycles(1, DEV)
+    try:
+        pe.pe_linear_stats(li.X, li.dY, "square")      # gives up; nobody has asked for the status yet
+    finally:
+        pe.pe_set_wait_limit_cycles(0, DEV)
+        pe.pe_set_path(pe.PATH_AUTO)
+    theta, m = theta0.clone(), torch.zeros_like(G)
+    pe.muon_step(theta, m, G, 4, lr=0.1, beta=0.9)
+    got = pe.pe_orthogonalize(G)
+    status, detail = pe.pe_get_async_status(DEV)
+    assert status == PE_ERR_TIMEOUT and 1 <= detail <= 4, (status, detail)
+    assert torch.equal(theta, stepped) and torch.equal(m, moved) and torch.equal(got, want)
