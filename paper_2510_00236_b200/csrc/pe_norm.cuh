@@ -10,6 +10,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "pe_sm100.cuh"
 
 namespace pe {
@@ -241,15 +243,21 @@ __device__ __forceinline__ void norm_fetch_aligned(uint32_t dst, const void* src
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(n), "r"(bar) : "memory");
 }
 
-// A thread's 8 features of a row in shared memory, as pairs: vector i is `offset[i]` bytes past byte `at`.  Vectors that are out of range have the offset of the
-// first one (norm_offsets): what they hold then is weighted with zero, or not written, by the caller.  Threads whose first vector is out of range are left out.
-template <typename T, int E>
+// A thread's 8 features of a row in shared memory, as pairs: vector i is `offset[i]` bytes past byte `at`.  Vectors that are out of range have offset 0
+// (norm_offsets), which only the first one has otherwise.  ZERO: they are zeros; else they hold the first one again, and the caller writes none of them.  (Weighting
+// what they hold with zero does not do in sums: an infinity there is NaN.)  Threads whose first vector is out of range are left out.
+template <typename T, int E, bool ZERO>
 __device__ __forceinline__ void norm_row_pairs(const uint8_t* shared, uint32_t at, const uint32_t (&offset)[NORM_COLS / E], uint64_t (&o)[NORM_COLS / 2]) {
   constexpr int NV = NORM_COLS / E;
   float f[NV][E];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const uint8_t* q = shared + (at + offset[i]);
+    if (ZERO && i > 0 && offset[i] == 0u) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[i][e] = 0.f;
+      continue;
+    }
     if constexpr (E == 8) {
       const uint4 v = *reinterpret_cast<const uint4*>(q);
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -265,18 +273,10 @@ __device__ __forceinline__ void norm_row_pairs(const uint8_t* shared, uint32_t a
 #pragma unroll
   for (int j = 0; j < NORM_COLS / 2; ++j) o[j] = sm100::f32x2_pack(f[2 * j / E][2 * j % E], f[(2 * j + 1) / E][(2 * j + 1) % E]);
 }
-// The vectors' offsets, and 1 or 0 for the features: in range or not.
 template <typename T, int E>
-__device__ __forceinline__ void norm_offsets(int G, int t, int cols, uint32_t (&offset)[NORM_COLS / E], uint64_t (&in)[NORM_COLS / 2]) {
-  float f[NORM_COLS / E];
+__device__ __forceinline__ void norm_offsets(int G, int t, int cols, uint32_t (&offset)[NORM_COLS / E]) {
 #pragma unroll
-  for (int i = 0; i < NORM_COLS / E; ++i) {
-    const bool inside = (i * G + t) * E < cols;
-    offset[i] = inside ? (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)) : 0u;
-    f[i] = inside ? 1.f : 0.f;
-  }
-#pragma unroll
-  for (int j = 0; j < NORM_COLS / 2; ++j) in[j] = sm100::f32x2_pack(f[2 * j / E], f[(2 * j + 1) / E]);
+  for (int i = 0; i < NORM_COLS / E; ++i) offset[i] = (i * G + t) * E < cols ? (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)) : 0u;
 }
 
 // s / d, with a reciprocal and a correction by the remainder: the quotient itself where it is a float, so that the mean of equal values is that value.
@@ -456,8 +456,10 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
   }
   const bool active = t * E < d;
   uint32_t offset[NV];
-  uint64_t inside[P];
-  norm_offsets<T, E>(G, t, d, offset, inside);
+  norm_offsets<T, E>(G, t, d, offset);
+  uint64_t inside[P];      // 1 or 0: features out of range do not deviate from the mean
+#pragma unroll
+  for (int j = 0; j < P; ++j) inside[j] = f32x2_pack(2 * j < E || offset[2 * j / E] != 0u ? 1.f : 0.f, 2 * j + 1 < E || offset[(2 * j + 1) / E] != 0u ? 1.f : 0.f);
   const float fd = (float)d, inv_d = 1.f / fd;
   int turn = 0, sl = 0;
   uint32_t phase = 0;
@@ -472,7 +474,8 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     __syncwarp();
     const uint32_t first = at + (E > 1 ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(x + (r0 + row0) * d) & 15));
     // rows behind the last one hold what was there before: their results are not written
-    auto pairs = [&](int k, uint64_t (&o)[P]) { norm_row_pairs<T, E>(smem, first + k * row_bytes, offset, o); };
+    auto pairs = [&](int k, uint64_t (&o)[P]) { norm_row_pairs<T, E, true>(smem, first + k * row_bytes, offset, o); };
+    auto pairs_written = [&](int k, uint64_t (&o)[P]) { norm_row_pairs<T, E, false>(smem, first + k * row_bytes, offset, o); };
     float mu[R], q[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) mu[k] = q[k] = 0.f;
@@ -483,7 +486,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
           uint64_t f[P], s2 = 0ull;
           pairs(k, f);
 #pragma unroll
-          for (int j = 0; j < P; ++j) s2 = E == 8 ? f32x2_add(s2, f[j]) : f32x2_fma(f[j], inside[j], s2);
+          for (int j = 0; j < P; ++j) s2 = f32x2_add(s2, f[j]);
           float lo, hi;
           f32x2_unpack(s2, lo, hi);
           mu[k] = lo + hi;
@@ -500,7 +503,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
 #pragma unroll
         for (int j = 0; j < P; ++j) {
           const uint64_t c = RMS ? f[j] : f32x2_add(f[j], m2);
-          s2 = f32x2_fma(E == 8 ? c : f32x2_mul(c, inside[j]), c, s2);
+          s2 = f32x2_fma(E == 8 || RMS ? c : f32x2_mul(c, inside[j]), c, s2);
         }
         float lo, hi;
         f32x2_unpack(s2, lo, hi);
@@ -521,7 +524,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     }
     auto write_row = [&](int k) {
       uint64_t f[P];
-      pairs(k, f);
+      pairs_written(k, f);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(q[k], q[k]);
       float o[NV][E];
 #pragma unroll
@@ -854,15 +857,11 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   float2 means[SUMMED ? 1 : R];
   const bool active = t * E < cols;      // a thread with features
   uint32_t offset[NV];
-  uint64_t inside[P];
-  norm_offsets<T, E>(G, t, cols, offset, inside);
-#pragma unroll
-  for (int j = 0; j < P; ++j)
-    if constexpr (E < 8) gain[j] = f32x2_mul(gain[j], inside[j]);      // features out of range have no part in the row's means
-  // this thread's features of row k of the slot, as pairs
-  auto pairs = [&](uint32_t tensor_at, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
+  norm_offsets<T, E>(G, t, cols, offset);
+  // this thread's features of row k of the slot, as pairs; summed: those out of range are zeros, so that they have no part in the row's means
+  auto pairs = [&](auto summed, uint32_t tensor_at, const T* tensor, long long row, int k, uint64_t (&o)[P]) {
     if constexpr (E == 1 && !WHOLE) tensor_at += (uint32_t)(reinterpret_cast<uintptr_t>(tensor + (row + k) * d + col0) & 15);
-    norm_row_pairs<T, E>(smem, tensor_at + k * row_bytes, offset, o);
+    norm_row_pairs<T, E, decltype(summed)::value>(smem, tensor_at + k * row_bytes, offset, o);
   };
   for (int b = 0; b < turns; ++b) {
     const int row0 = b * R;
@@ -891,8 +890,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     for (int k = 0; k < SUMS; ++k) s[k] = 0.f;
     auto sums_of = [&](int k, float mean_k, float rstd_k, float& wc, float& ws) {
       uint64_t fx[P], fy[P], s0 = 0ull, s1 = 0ull;
-      pairs(at_x, x, r0 + row0, k, fx);
-      pairs(at_y, dy, r0 + row0, k, fy);
+      pairs(std::integral_constant<bool, SUMMED>{}, at_x, x, r0 + row0, k, fx);
+      pairs(std::integral_constant<bool, SUMMED>{}, at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mean_k, -mean_k), r2 = f32x2_pack(rstd_k, rstd_k);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
@@ -1039,8 +1038,8 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
         if constexpr (!RMS) k0 = -rs[k] * means[k].y;
       }
       uint64_t fx[P], fy[P];
-      pairs(at_x, x, r0 + row0, k, fx);
-      pairs(at_y, dy, r0 + row0, k, fy);
+      pairs(std::false_type{}, at_x, x, r0 + row0, k, fx);
+      pairs(std::false_type{}, at_y, dy, r0 + row0, k, fy);
       const uint64_t m2 = f32x2_pack(-mu[k], -mu[k]), r2 = f32x2_pack(rs[k], rs[k]), k02 = f32x2_pack(k0, k0), k12 = f32x2_pack(k1, k1);
       float o[NV][E];
 #pragma unroll

@@ -62,3 +62,55 @@ def test_rows_at_the_ends_of_a_buffer():
         pe.pe_norm_forward(views[0], gain, bias, out=views[3])
         for t in store:
             assert torch.isnan(t[:shift]).all() and torch.isnan(t[shift + n:]).all() and not torch.isnan(t[shift:shift + n]).any()
+
+
+def _same_pattern(got, want):
+    """NaN, and infinities of either sign, at the same places."""
+    got, want = got.double(), want.double()
+    return torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got == float("inf"), want == float("inf")) and torch.equal(got == -float("inf"), want == -float("inf"))
+
+
+# many rows (the forward ring) and few; threads whose last features are out of range, aligned fp32 rows among them; slices of rows
+INFINITE = [(13001, 333, "bf16"), (13001, 333, "fp32"), (40, 333, "fp32"), (9, 100, "fp32"), (70, 1004, "fp32"), (5, 4609, "bf16"), (5, 5004, "fp32"), (1, 33001, "fp32"), (200001, 21, "bf16")]
+
+
+@pytest.mark.parametrize("rows,d,dtype", INFINITE)
+def test_infinities_under_rms(rows, d, dtype):
+    """An infinity in a row makes its rstd zero: that feature is NaN, every other one the bias, whichever feature it is."""
+    x, _, gain, bias = _rows(1, rows, d, DT[dtype], d)
+    x = x[0]
+    where = {k * (rows // 5): c for k, c in enumerate((0, 1, d // 2, d - 2, d - 1)) if rows >= 5} or {0: d // 2}
+    clean, _, r0 = pe.pe_norm_forward(x, gain, bias, kind="rms", eps=EPS)
+    for row, c in where.items():
+        x[row, c] = -float("inf") if c & 1 else float("inf")
+    y, _, r = pe.pe_norm_forward(x, gain, bias, kind="rms", eps=EPS)
+    for row, c in where.items():
+        want = bias.to(DT[dtype]).clone()
+        want[c] = float("nan")
+        assert float(r[row]) == 0.0 and torch.equal(torch.isnan(y[row]), torch.isnan(want)) and torch.equal(y[row].nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+        y[row], r[row] = clean[row], r0[row]
+    assert torch.equal(y, clean) and torch.equal(r, r0)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("rows,d,dtype", INFINITE)
+def test_infinite_gradients(rows, d, dtype, kind):
+    """dx where dy holds an infinity: infinite or NaN just where the formula is."""
+    x, dy, gain, _ = _rows(1, rows, d, DT[dtype], d + 1)
+    mean, rstd = _stats(x, kind)
+    dy[0, 0, 0] = float("inf")
+    dy[0, rows // 2, d - 1] = -float("inf")
+    dy[0, rows - 1, d // 2] = float("inf")
+    dx, gain_sum, *_ = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind)
+    hit = sorted({0, rows // 2, rows - 1})
+    xs, ds, r = x[0, hit].double(), dy[0, hit].double(), rstd[0, hit, None].double()
+    h = (xs - (mean[0, hit, None].double() if kind == "layer" else 0.0)) * r
+    w = ds * gain.double()
+    want = r * (w - h * (w * h).mean(1, keepdim=True) - (w.mean(1, keepdim=True) if kind == "layer" else 0.0))
+    assert _same_pattern(dx[0, hit], want)
+    others = torch.ones(rows, dtype=torch.bool, device=DEV)
+    others[hit] = False
+    assert torch.isfinite(dx[0, others]).all()
+    finite = torch.ones(d, dtype=torch.bool, device=DEV)
+    finite[[0, d - 1, d // 2]] = False
+    assert torch.isfinite(gain_sum[finite]).all() and not torch.isfinite(gain_sum[~finite]).any()
