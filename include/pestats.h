@@ -305,7 +305,7 @@ pe_status_t pe_token_sqstats_static(const void* X, const void* dY, int B, int T,
  * (The paper leaves such parameters to its general per-example form, which needs their gradient per example; Appendix E.2.2's
  * transformer normalises before every block.)
  * x, y: bf16 [rows, d], 16-byte aligned, not overlapping; gain, bias: fp32 [d], 4-byte aligned, NULL for ones / zeros; mean, rstd: fp32 [rows], 4-byte
- * aligned, what pe_norm_backward reads; NULL to skip (PE_NORM_RMS writes no mean).  rows >= 0, d >= 1, rows * d < 2^40, eps >= 0.
+ * aligned, what pe_norm_backward reads; NULL to skip (PE_NORM_RMS writes no mean).  rows >= 0, 1 <= d < 2^31 - 1024, rows * d < 2^40, eps >= 0.
  * Sums are fp32: the mean first, then the squared deviations from it.  y is rounded once.  An unknown kind is PE_ERR_PHI.  After PE_ERR_TIMEOUT (see
  * pe_get_async_status) some rows of y, mean and rstd are as they were before.
  */
@@ -322,7 +322,7 @@ pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* 
  *     dx = rstd * (w - xh * mean(w * xh) - mean(w))        (PE_NORM_RMS: without the last term)
  *     G_b = sum_{t<T} dy[b,t] * xh[b,t],   H_b = sum_{t<T} dy[b,t]            (vectors of d)
  *     gain_sum = sum_b G_b,  gain_stat = sum_b phi(G_b),  bias_sum = sum_b H_b,  bias_stat = sum_b phi(H_b).
- * x, dy, dx: bf16 [B, T, d], 16-byte aligned; mean (PE_NORM_LAYER only), rstd: fp32 [B, T], what the forward pass wrote; gain as
+ * x, dy, dx: bf16 [B, T, d], 16-byte aligned, d <= 2^28; mean (PE_NORM_LAYER only), rstd: fp32 [B, T], what the forward pass wrote; gain as
  * there.  Outputs: fp32 [d], 4-byte aligned, overwritten, or added to where accumulate != 0 (micro-batches); any of dx and the
  * four may be NULL to skip it (not all).  dx must not overlap x or dy.
  * workspace: device memory, 256-byte aligned, pe_norm_backward_workspace_bytes(B * T, d) bytes, contents undefined afterwards.

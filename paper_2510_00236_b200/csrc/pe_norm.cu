@@ -27,7 +27,7 @@ struct ForwardPlan {
 };
 // A power of two of lanes per row while one vector each covers it, then a warp with up to 8 vectors each, then several warps.
 static ForwardPlan plan_forward(int d, int E) {
-  const int vectors = (d + E - 1) / E;
+  const int vectors = (d - 1) / E + 1;
   ForwardPlan p = {32, 1, 256};
   if (vectors <= 32) {
     p.G = 1;
@@ -39,7 +39,7 @@ static ForwardPlan plan_forward(int d, int E) {
     p.G = (vectors + 32 * p.nv - 1) / (32 * p.nv) * 32;
   } else {
     p.G = 0;
-    p.threads = 1024;
+    p.threads = NORM_WIDE_THREADS;
     return p;
   }
   p.threads = p.G * std::max(1, 256 / p.G);
@@ -48,7 +48,7 @@ static ForwardPlan plan_forward(int d, int E) {
 
 // Threads to a row where each has 8 of its features: a power of two up to a warp, whole warps above.
 static int row_threads(int d) {
-  const int threads = (d + NORM_COLS - 1) / NORM_COLS;
+  const int threads = (d - 1) / NORM_COLS + 1;
   if (threads > 32) return (threads + 31) / 32 * 32;
   int G = 1;
   while (G < threads) G *= 2;
@@ -94,12 +94,14 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
 }
 
 static bool norm_size_ok(long long rows, int d) { return rows >= 0 && d >= 1 && rows < (1ll << 40) && (rows == 0 || rows <= ((1ll << 40) - 1) / d); }
+// (byte offsets of a turn's rows are 32 bits in the backward pass: three bf16 rows or one of fp32 before the last one)
+constexpr int NORM_MAX_BACKWARD_D = 1 << 28;
 static bool kind_ok(pe_norm_t kind) { return kind == PE_NORM_LAYER || kind == PE_NORM_RMS; }
 
 template <typename T>
 static pe_status_t forward_impl(const T* x, const float* gain, const float* bias, long long rows, int d, pe_norm_t kind, float eps, T* y, float* mean,
                                 float* rstd, cudaStream_t st) {
-  if (!norm_size_ok(rows, d) || !(eps >= 0.f)) return PE_ERR_DIM;
+  if (!norm_size_ok(rows, d) || d > NORM_MAX_FORWARD_D || !(eps >= 0.f)) return PE_ERR_DIM;
   if (!kind_ok(kind)) return PE_ERR_PHI;
   if (rows > 0 && (!x || !y)) return PE_ERR_NULL;
   const size_t al = sizeof(T) == 2 ? 16 : 4;
@@ -160,7 +162,7 @@ static pe_status_t launch_rows(const T* x, const T* dy, T* dx, const NormBackwar
   auto kernel = norm_backward_kernel<T, E, RMS, KINDS, MODE, SHORT>;
   static std::atomic<int> allowed[MAX_DEVICES];
   const pe_status_t rc = allow_smem(kernel, allowed, smem);
-  return rc != PE_OK ? rc : launch_dependent(kernel, dim3(p.blocks, p.slabs), p.G * p.groups, smem, st, x, dy, dx, a);
+  return rc != PE_OK ? rc : launch_dependent(kernel, MODE == NORM_SLAB ? dim3(p.slabs, p.blocks) : dim3(p.blocks), p.G * p.groups, smem, st, x, dy, dx, a);
 }
 template <typename T, int E, bool RMS, int KINDS, bool SHORT>
 static pe_status_t launch_cluster(const T* x, const T* dy, T* dx, NormBackward& a, BackwardPlan& p, int smem, cudaStream_t st) {
@@ -221,7 +223,7 @@ template <typename T>
 static pe_status_t backward_impl(const T* x, const T* dy, const float* gain, const float* mean, const float* rstd, const int* offsets, bool packed, int B,
                                  int T_, long long rows, int d, pe_norm_t kind, pe_phi_t phi, int accumulate, T* dx, float* gain_sum, float* gain_stat,
                                  float* bias_sum, float* bias_stat, void* workspace, size_t workspace_bytes, cudaStream_t st) {
-  if (B < 0 || T_ < 0 || !norm_size_ok(rows, d) || (packed && rows >= (1ll << 31))) return PE_ERR_DIM;
+  if (B < 0 || T_ < 0 || !norm_size_ok(rows, d) || d > NORM_MAX_BACKWARD_D || (packed && rows >= (1ll << 31))) return PE_ERR_DIM;
   if (!kind_ok(kind) || (phi != PE_PHI_IDENTITY && phi != PE_PHI_SQUARE && phi != PE_PHI_SIGN)) return PE_ERR_PHI;
   const bool empty = B == 0 || rows == 0;
   if (!empty && (!x || !dy || !rstd || (kind == PE_NORM_LAYER && !mean) || (packed && !offsets))) return PE_ERR_NULL;
@@ -287,7 +289,7 @@ pe_status_t pe_norm_forward_f32(const float* x, const float* gain, const float* 
 }
 
 size_t pe_norm_backward_workspace_bytes(long long rows, int d) {
-  if (!norm_size_ok(rows, d) || rows == 0) return 0;
+  if (!norm_size_ok(rows, d) || d > NORM_MAX_BACKWARD_D || rows == 0) return 0;
   return plan_backward(rows, d, 2, NORM_SM_COUNT).bytes;
 }
 

@@ -557,9 +557,11 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
   }
 }
 
-// Rows too wide for a block's registers: three passes over the row, the later ones from L2.
+// Rows too wide for a block's registers: three passes over the row, the later ones from L2.  (A feature's number is an int, NORM_MAX_FORWARD_D keeps it below 2^31 a
+// step behind the row's end too; with unsigned ones 64 x 64 x 40000 bf16 took 529 us and 352.)
+constexpr int NORM_WIDE_THREADS = 1024, NORM_MAX_FORWARD_D = INT32_MAX - NORM_WIDE_THREADS;
 template <typename T, bool RMS>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(NORM_WIDE_THREADS)
 norm_forward_wide_kernel(const T* __restrict__ x, const float* __restrict__ gain, const float* __restrict__ bias, long long rows, int d, float eps,
                          T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd) {
   __shared__ float slots[2 * NORM_MAX_WARPS];
@@ -692,7 +694,7 @@ struct NormEnds {
 
 // KINDS: 1 for the gain alone, 2 with the bias.
 // NORM_WHOLE: a group has the whole row and finds the row's two means itself.  NORM_CLUSTER: wider rows are cut into slices for the blocks of a cluster,
-// which exchange their sums by way of each other's shared memory.  NORM_SLAB: wider still; blockIdx.y picks the features and row_means has the means.
+// which exchange their sums by way of each other's shared memory.  NORM_SLAB: wider still; blockIdx.x picks the features (a grid's y has 65535 at most) and row_means has the means.
 //
 // A worker's rows come through a ring in shared memory, NORM_STAGES slots of R rows, filled by bulk copies that the group's first thread issues two slots
 // ahead: 128 KB in flight on an SM without a register spent on them, whatever the rows' alignment.  (With the next row's loads in registers,
@@ -717,9 +719,10 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   __shared__ __align__(16) float exchanged[MODE == NORM_CLUSTER ? 2 : 1][MODE == NORM_CLUSTER ? NORM_MAX_CLUSTER : 1][SUMS];      // the blocks' sums, of two turns
   __shared__ uint64_t exchange_bar[2];
   const int G = p.G, d = p.d, group = threadIdx.x / G, t = threadIdx.x - group * G, groups = blockDim.x / G, threads = blockDim.x;
-  const int rank = MODE == NORM_CLUSTER ? (int)cluster_ctarank() : 0, block = MODE == NORM_CLUSTER ? (int)blockIdx.x / p.cluster : (int)blockIdx.x;
-  const int blocks = MODE == NORM_CLUSTER ? (int)gridDim.x / p.cluster : (int)gridDim.x;
-  const int col0 = WHOLE ? 0 : (MODE == NORM_CLUSTER ? rank : (int)blockIdx.y) * G * NORM_COLS, cols = WHOLE ? d : max(0, min(d - col0, G * NORM_COLS));
+  const int rank = MODE == NORM_CLUSTER ? (int)cluster_ctarank() : MODE == NORM_SLAB ? (int)blockIdx.x : 0;      // the slice of a row
+  const int block = MODE == NORM_CLUSTER ? (int)blockIdx.x / p.cluster : MODE == NORM_SLAB ? (int)blockIdx.y : (int)blockIdx.x;
+  const int blocks = MODE == NORM_CLUSTER ? (int)gridDim.x / p.cluster : MODE == NORM_SLAB ? (int)gridDim.y : (int)gridDim.x;
+  const int col0 = rank * G * NORM_COLS, cols = WHOLE ? d : max(0, min(d - col0, G * NORM_COLS));
   const size_t slot = norm_slot_bytes(R, WHOLE ? d : G * NORM_COLS, sizeof(T), WHOLE);
   // [group][stage][x, dy], then a barrier per group and stage
   uint8_t* ring = smem + (size_t)group * S * 2 * slot;
@@ -820,7 +823,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
   // [head, then tot, stat unless SHORT][kind][feature of a thread][thread]; written by the thread that reads it
   constexpr int KEPT = KINDS * NORM_COLS;
-  float* const heads = p.heads + ((size_t)((MODE == NORM_CLUSTER ? rank : (int)blockIdx.y) * blocks + block) * (SHORT ? 1 : 3) * KEPT) * threads + threadIdx.x;
+  float* const heads = p.heads + (((size_t)rank * blocks + block) * (SHORT ? 1 : 3) * KEPT) * threads + threadIdx.x;
   if constexpr (!SHORT) {
 #pragma unroll 4
     for (int k = KEPT; k < 3 * KEPT; ++k) heads[(size_t)k * threads] = 0.f;

@@ -66,3 +66,37 @@ def test_two_calls_at_once_on_two_streams():
     for k in range(2):
         for one in got[k]:
             assert all(torch.equal(a, b) for a, b in zip(one, want[k]))
+
+
+def test_rows_of_more_slices_than_a_grid_is_high():
+    """65537 slices of 2048 features."""
+    B, T, d = 2, 1, 65536 * 2048 + 8
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    x, dy = (torch.empty(B, T, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    mean, rstd = _stats(x, "layer")
+    got = pe.pe_norm_backward(x, dy, None, mean, rstd, "square")
+    assert pe.pe_get_async_status(DEV) == (0, 0)
+    _check_backward(got, x, dy, None, mean, rstd, [0, 1, 2], "square", "layer")
+
+
+def test_the_widest_row_forward():
+    """2^31 - 1025 features, the widest that are taken: a thread's last step ends just below 2^31.  Sums are over 2^21 terms of a thread, added one after the other, then 37 more."""
+    d, part = (1 << 31) - 1025, 1 << 27
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    x = torch.empty(1, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    y, mean, rstd = pe.pe_norm_forward(x, eps=EPS)
+    pieces = [slice(at, min(d, at + part)) for at in range(0, d, part)]
+    mu = sum(float(x[0, p].double().sum()) for p in pieces) / d
+    size = sum(float(x[0, p].double().abs().sum()) for p in pieces) / d
+    var = sum(float((x[0, p].double() - mu).square().sum()) for p in pieces) / d
+    k = (1 << 21) + 40
+    mu_off = U * k * size
+    r = (var + EPS) ** -0.5
+    r_off = r * (0.5 * (U * k * var + mu_off ** 2) / (var + EPS) + 4 * U)
+    assert abs(float(mean) - mu) <= mu_off and abs(float(rstd) - r) <= r_off
+    for p in pieces:
+        want = (x[0, p].double() - mu) * r
+        off = mu_off * r + want.abs() * (r_off / r + 3 * U)
+        assert_within("y", y[0, p], want, off, half_step(torch.bfloat16))

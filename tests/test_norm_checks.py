@@ -107,3 +107,17 @@ def test_binding_refuses_what_the_library_cannot_see():
         pe.pe_norm_forward(x)
     with pytest.raises(pe.PestatsError):
         pe.pe_norm_backward(x, x.clone(), None, r, r, "square")
+
+
+def test_rows_too_wide_are_refused(lib, p16):
+    """Before anything is enqueued; the widest that is taken passes on to the workspace, or to the device that is missing here."""
+    for f in (lib.pe_norm_backward, lib.pe_norm_backward_f32):
+        for d, refused in (((1 << 28) + 1, True), ((1 << 31) - 1, True), (1 << 28, False), (65535 * 2048 + 8, False)):
+            status = f(p16, p16, None, p16, p16, 1, 1, d, 0, 1, 0, p16, None, None, None, None, p16, 1 << 10, None)
+            assert (status == 2) == refused, d
+    for f in (lib.pe_norm_forward, lib.pe_norm_forward_f32):
+        for d, refused in (((1 << 31) - 1024, True), ((1 << 31) - 1, True), ((1 << 31) - 1025, False)):
+            assert (f(p16, None, None, 1, d, 0, 1e-5, p16, None, None, None) == 2) == refused, d
+    need = pe.pe_norm_backward_workspace_bytes
+    assert need(1, (1 << 28) + 1) == 0 and need(1, (1 << 31) - 1) == 0
+    assert need(1, 1 << 28) >= 8 * 4 * (1 << 28)
