@@ -62,15 +62,17 @@ static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain,
   // The ring where gain and bias out of L1 would hold rows up (16-bit rows of 1024 features or more: 256 x 1024 x 2048, 389 us against 563; 64 x 256 x 512, 11.4 and
   // 11.2) or single features would (256 x 256 x 333, 49 and 128); fp32 rows go faster without (64 x 256 x 1024, 26.7 and 23.6), and so do few rows
   // (8 x 256 x 1024, 7.0 and 5.8).
-  if (ring_G <= NORM_MAX_THREADS && rows * d >= (1ll << 22) && (E == 1 || (sizeof(T) == 2 && d >= 1024))) {
-    const int groups = std::max(1, 256 / ring_G), threads = ring_G * groups, smem = (int)(groups * NORM_STAGES * (norm_slot_bytes(norm_rows<T>(), d, sizeof(T), true) + 8));
-    const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 4096)));
-    const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
-    auto kernel = norm_forward_ring_kernel<T, E, RMS>;
-    static std::atomic<int> allowed[MAX_DEVICES];
-    const pe_status_t rc = allow_smem(kernel, allowed, smem);
-    if (rc != PE_OK) return rc;
-    return launch_dependent(kernel, dim3((unsigned)blocks), threads, smem, st, x, gain, bias, rows, d, eps, y, mean, rstd, ring_G, wide, di->status_ptr);
+  if constexpr (E == 1 || sizeof(T) == 2) {
+    if (ring_G <= NORM_MAX_THREADS && rows * d >= (1ll << 22) && (E == 1 || d >= 1024)) {
+      const int groups = std::max(1, 256 / ring_G), threads = ring_G * groups, smem = (int)(groups * NORM_STAGES * (norm_slot_bytes(norm_rows<T>(), d, sizeof(T), true) + 8));
+      const long long most = (long long)di->sm_count * std::max(1, std::min((E == 1 ? 512 : 1024) / threads, 220 * 1024 / (smem + 4096)));
+      const long long blocks = std::max(1ll, std::min(most, rows / (2ll * norm_rows<T>() * groups)));      // two turns at least
+      auto kernel = norm_forward_ring_kernel<T, E, RMS>;
+      static std::atomic<int> allowed[MAX_DEVICES];
+      const pe_status_t rc = allow_smem(kernel, allowed, smem);
+      if (rc != PE_OK) return rc;
+      return launch_dependent(kernel, dim3((unsigned)blocks), threads, smem, st, x, gain, bias, rows, d, eps, y, mean, rstd, ring_G, wide, di->status_ptr);
+    }
   }
   const ForwardPlan p = plan_forward(d, E);
   if (p.G == 0)
