@@ -524,8 +524,12 @@ int pe_tile_order_band(int d_in, int d_out, int tile_cols, int batch_slices, int
  *     chunks are dealt out evenly, over how many pairs, and pairs in all.
  *   PE_PLAN_NORMS (pe_example_sqnorms on the tensor cores): slices of the batch, their examples if a pair of thread blocks takes tiles and slices in turn (else 0),
  *     slices that the tile order is chosen for.
+ *   PE_PLAN_ORTHOGONALIZE (pe_orthogonalize and muon_step on B matrices [d_out, d_in]; outputs: the product, 0 X X^T, 1 the polynomial's, 2 the one with X; T and
+ *     sm_count do not matter): width of its tiles (0: no products, a block takes a matrix through all steps), slices of the contraction index, tiles of a
+ *     matrix, steps that are taken at a time.
  * PE_ERR_DIM for arguments out of range. */
-typedef enum { PE_PLAN_SHORT = 0, PE_PLAN_SIMT_STATS = 1, PE_PLAN_SIMT_TOKEN = 2, PE_PLAN_SIMT_NORMS = 3, PE_PLAN_TOKEN = 4, PE_PLAN_NORMS = 5 } pe_plan_t;
+typedef enum { PE_PLAN_SHORT = 0, PE_PLAN_SIMT_STATS = 1, PE_PLAN_SIMT_TOKEN = 2, PE_PLAN_SIMT_NORMS = 3, PE_PLAN_TOKEN = 4, PE_PLAN_NORMS = 5,
+               PE_PLAN_ORTHOGONALIZE = 6 } pe_plan_t;
 pe_status_t pe_plan_query(int what /* pe_plan_t */, int outputs, int B, int T, int d_in, int d_out, int sm_count, long long* plan);
 /* Number of kernels the library has launched since load (or since the last reset to 0 via
  * pe_reset_launch_count). */

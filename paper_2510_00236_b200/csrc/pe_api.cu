@@ -2100,6 +2100,7 @@ pe_status_t pe_plan_query(int what, int outputs, int B, int T, int d_in, int d_o
       plan[0] = p.slices; plan[1] = p.examples; plan[2] = p.order_slices;
       return PE_OK;
     }
+    case PE_PLAN_ORTHOGONALIZE: return pe::ns_plan_query(outputs, B, d_out, d_in, plan);
     default: return PE_ERR_DIM;
   }
 }

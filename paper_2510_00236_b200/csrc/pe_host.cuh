@@ -33,6 +33,7 @@ EncodeTiledFn encode_fn();
 // pe_set_wait_limit_cycles for the kernels of the other translation units (each has its own copy of the limit)
 pe_status_t ns_set_wait_limit(long long cycles);
 pe_status_t norm_set_wait_limit(long long cycles);
+pe_status_t ns_plan_query(int product, int count, int rows, int cols, long long* plan);      // PE_PLAN_ORTHOGONALIZE
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }

@@ -228,6 +228,15 @@ static pe_status_t orthogonalize_impl(const void* G, int bf16, int count, int ro
   return newton_schulz(di, s, count, rows, cols, steps, p, static_cast<char*>(workspace), st);
 }
 
+pe_status_t ns_plan_query(int product, int count, int rows, int cols, long long* plan) {
+  if (product < 0 || product > 2 || !ns_size_ok(count, rows, cols)) return PE_ERR_DIM;
+  const NsLayout l = ns_layout(count, rows, cols);
+  const bool small = ns_is_small(l);
+  const NsPlan& p = product == 0 ? l.gram : product == 1 ? l.poly : l.apply;
+  plan[0] = small ? 0 : p.nt; plan[1] = small ? 0 : p.splits; plan[2] = small ? 0 : p.units; plan[3] = !small && l.pairs ? 2 : 1;
+  return PE_OK;
+}
+
 pe_status_t ns_set_wait_limit(long long cycles) {
   if (cudaMemcpyToSymbol(sm100::g_wait_cycle_limit, &cycles, sizeof cycles) != cudaSuccess) { cudaGetLastError(); return PE_ERR_CUDA; }
   return PE_OK;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2510_00236_b200 as pe
-from test_gpu_muon import DEV, U, _noise, _rel, exact, tolerance
+from test_gpu_muon import A, B_, C, DEV, U, _noise, _rel, exact, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,75 @@ def test_waits_that_run_out_leave_parameters_alone():
     assert pe.pe_get_async_status(DEV) == (0, 0) and not torch.equal(theta, start)
     again = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square")
     assert all(torch.equal(a, b) for a, b in zip(want, again)) and torch.equal(pe.pe_norm_forward(x, gain)[0], y)
+
+
+# tiles of every width for every product, X X^T in slices for every width, one step and two at a time (test_muon_checks.py looks the plans over)
+PRECISE = [(1, 300, 300), (1, 512, 2048), (1, 256, 4096), (1, 2048, 2048), (1, 1537, 1601), (2, 1100, 1100), (1, 8192, 2048), (1, 512, 32768), (12, 600, 600), (12, 601, 1999),
+           (1, 1000, 8000), (1, 2049, 3000), (80, 130, 300), (1, 65, 129), (12, 449, 272), (2, 655, 2586), (12, 322, 1069), (20, 590, 326), (2, 962, 2231), (1, 1427, 2202),
+           (1, 3078, 514), (40, 129, 129), (40, 143, 74)]
+
+
+def _halves(v):
+    """Operands of 11 bits, scaled as the kernels scale theirs."""
+    return (v * 4096.0).half().double() / 4096.0
+
+
+def sensitivity(G, steps=5):
+    """What the iteration makes of operands rounded to 11 bits, relative to the result and to the rounding of 2^-11 (about 3 for noise, 60 where few directions dominate)."""
+    X = G.double() / torch.linalg.vector_norm(G.double())
+    X = X.T if X.shape[0] > X.shape[1] else X
+    Y = X
+    eye = torch.eye(X.shape[0], dtype=X.dtype, device=X.device)
+    for _ in range(steps):
+        S = X @ X.T
+        X = (A * eye + B_ * S + C * (S @ S)) @ X
+        y = _halves(Y)
+        S = y @ y.T
+        s = _halves(S)
+        Y = _halves(A * eye + B_ * s + C * (s @ s)) @ y
+    return float((X - Y).norm() / X.norm()) * 2.0 ** 11
+
+
+def precision(G, paired, steps=5):
+    """Relative error of the Frobenius norm of what the kernels' arithmetic may cost.  Two halves leave 2^-22 of an operand where one leaves 2^-11, at the same places: the
+    sensitivity times 2^-22; lo lo, which is left out, is as much at most.  The tensor cores add by truncation, an accumulator takes 64 values in four
+    instructions (the cross terms before are 2^-11 of them): 2.5 * 2^-23 of a sum at most, and as much again for the terms within an instruction.  Off by a relative
+    e on one side, as the diagonals of A and A A are, whose terms have one sign, a step is off by (|b| s^3 + 3 |c| s^5) e, 12 e at s = 1, where the rounding of
+    operands costs about 1.5 of its unit: 12 * 2.5 / 1.5 = 20 sensitivities.  Together 22, say 24; with two steps at a time, five more products, twice that."""
+    return (48 if paired else 24) * sensitivity(G, steps) * 2.0 ** -22
+
+
+@pytest.mark.parametrize("spread", [0.0, 0.3])
+@pytest.mark.parametrize("count,rows,cols", PRECISE)
+def test_operands_of_22_bits(count, rows, cols, spread):
+    """The bounds of the other tests leave room for operands of 11 bits; these are for the arithmetic as it is."""
+    G = _noise(count, rows, cols, rows + 3 * cols, spread)
+    paired = pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, 0, count, 1, cols, rows, 148)[3] == 2
+    got = pe.pe_orthogonalize(G)
+    assert pe.pe_get_async_status(DEV) == (0, 0)
+    for k in sorted({0, count // 2, count - 1}):
+        assert _rel(got[k], exact(G[k])) <= precision(G[k], paired), k
+    if count > 1:      # every matrix by itself, in tiles of another width perhaps
+        for k in range(count):
+            assert _rel(got[k], pe.pe_orthogonalize(G[k]).double()) <= 2 * precision(G[k], True), k
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 2048, 2048), (1, 8192, 2048), (12, 601, 1999), (1, 512, 2048)])
+def test_muon_step_with_operands_of_22_bits(count, rows, cols):
+    theta, m, sum_g = torch.zeros(count, rows, cols, device=DEV), _noise(count, rows, cols, 7) * 0.1, _noise(count, rows, cols, 8)
+    m0 = m.double()
+    paired = pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, 0, count, 1, cols, rows, 148)[3] == 2
+    pe.muon_step(theta, m, sum_g, 4, lr=1.0, beta=0.9, update_scale=1.0)
+    for k in range(count):
+        g = sum_g[k].double() / 4
+        direction = 0.1 * g + 0.9 * (0.9 * m0[k] + 0.1 * g)
+        # the direction is rounded to fp32 a few times on its way: 6 * 2^-24 of each value, one more and a half of the operands' units
+        assert _rel(-theta[k], exact(direction)) <= 1.1 * precision(direction, paired), k
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 300, 4100), (12, 601, 1999), (1, 158, 1204), (2, 1001, 999)])
+def test_what_the_workspace_holds_before_does_not_matter(count, rows, cols):
+    G = _noise(count, rows, cols, 9)
+    need = pe.pe_orthogonalize_workspace_bytes(count, rows, cols)
+    got = [pe.pe_orthogonalize(G, workspace=torch.full((need,), fill, dtype=torch.uint8, device=DEV)) for fill in (0, 255, 127)]
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2]) and torch.isfinite(got[0]).all()

@@ -75,3 +75,25 @@ def test_binding_refuses_what_the_library_cannot_see():
         pe.muon_step(G, G.clone(), G.clone(), 4, lr=0.1, beta=0.9, theta_lp=G.clone())
     with pytest.raises(pe.PestatsError):                # tensors on the CPU
         pe.pe_orthogonalize(G)
+
+
+def test_the_shapes_whose_precision_is_tested_take_every_kind_of_product(lib):
+    """Widths of tiles and slices follow an estimate of the time: should it change, the list of shapes has to change with it."""
+    from test_gpu_muon_pairs import PRECISE
+    taken = set()
+    for count, rows, cols in PRECISE:
+        for product in range(3):
+            width, slices, _, at_a_time = pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, product, count, 1, cols, rows, 148)
+            taken.add((product, at_a_time, width, slices > 1))
+    assert taken >= {(product, at_a_time, width, False) for product in range(3) for at_a_time in (1, 2) for width in (64, 128, 256)}
+    # X X^T in slices; the other products never are
+    assert taken >= {(0, 1, 64, True), (0, 1, 256, True), (0, 2, 64, True), (0, 2, 128, True), (0, 2, 256, True)}
+    assert not any(sliced for product, _, _, sliced in taken if product)
+
+
+def test_plan_queries_of_the_orthogonalised_update(lib):
+    for bad in ((3, 1, 64, 64), (-1, 1, 64, 64), (0, 65536, 1, 1), (0, 1, 1 << 30, 1 << 30)):
+        with pytest.raises(pe.PestatsError):
+            pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, bad[0], bad[1], 1, bad[3], bad[2], 148)
+    assert pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, 0, 3, 1, 128, 64, 148)[0] == 0 and pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, 0, 3, 1, 64, 128, 148)[0] == 0
+    assert pe.pe_plan_query(pe.PLAN_ORTHOGONALIZE, 0, 1, 1, 129, 64, 148)[0] > 0
