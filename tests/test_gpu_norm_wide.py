@@ -114,3 +114,30 @@ def test_infinite_gradients(rows, d, dtype, kind):
     finite = torch.ones(d, dtype=torch.bool, device=DEV)
     finite[[0, d - 1, d // 2]] = False
     assert torch.isfinite(gain_sum[finite]).all() and not torch.isfinite(gain_sum[~finite]).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("B,T,d", [(3, 3001, 8192), (1100, 3, 12292), (2, 1200, 32768), (5, 601, 24003)])
+def test_slices_that_exchange_sums_over_dozens_of_turns(B, T, d, dtype, kind):
+    """4 bf16 rows or 2 fp32 ones a turn, 15 to 74 clusters: at least 24 turns, so that the ring and both words of the exchange are used over and over.
+    (A cluster's sums go over at most 3000 / 15 rows and the joins, fewer than the additions that the bound is made for.)"""
+    x, dy, gain, _ = _rows(B, T, d, DT[dtype], d + B)
+    mean, rstd = _stats(x, kind)
+    got = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind)
+    assert pe.pe_get_async_status(DEV) == (0, 0)
+    _check_backward(got, x, dy, gain, mean, rstd, list(range(0, B * T + 1, T)), "square", kind)
+    for _ in range(3):
+        again = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", kind=kind)
+        assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+
+
+@pytest.mark.parametrize("B,T,d", [(3, 40, 64), (700, 33, 320), (40, 100, 2048), (5, 70, 8192), (3, 50, 40000)])
+def test_what_the_workspace_holds_before_does_not_matter(B, T, d):
+    x, dy, gain, _ = _rows(B, T, d, torch.bfloat16, 11)
+    mean, rstd = _stats(x, "layer")
+    need = pe.pe_norm_backward_workspace_bytes(B * T, d)
+    got = [pe.pe_norm_backward(x, dy, gain, mean, rstd, "square", workspace=torch.full((need,), fill, dtype=torch.uint8, device=DEV)) for fill in (0, 255, 127)]
+    for one in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], one))
+    assert all(torch.isfinite(t).all() for t in got[0])
