@@ -121,3 +121,12 @@ def test_rows_too_wide_are_refused(lib, p16):
     need = pe.pe_norm_backward_workspace_bytes
     assert need(1, (1 << 28) + 1) == 0 and need(1, (1 << 31) - 1) == 0
     assert need(1, 1 << 28) >= 8 * 4 * (1 << 28)
+
+
+def test_workspace_of_rows_wider_than_a_cluster(lib):
+    """Beyond 32768 features the two means of every row are kept there, 8 bytes; below, nothing grows with the rows once every SM has its blocks."""
+    need = pe.pe_norm_backward_workspace_bytes
+    for d in (32776, 40000, 100001):
+        assert need(3000000, d) - need(1000000, d) == 16000000
+    for d in (64, 2048, 4096, 8192, 32768):
+        assert need(3000000, d) == need(1000000, d)
