@@ -156,3 +156,30 @@ def test_sums_of_narrow_rows_repeat_bit_for_bit(B, T, d, dtype):
         again = pe.pe_norm_backward(x, dy, gain, mean, rstd, "square")
         wrong += not all(torch.equal(a, b) for a, b in zip(first, again))
     assert wrong == 0
+
+
+# three slots of the forward ring take between 47.5 and 48 KB
+BAND = [("bf16", 121), ("bf16", 249), ("fp32", 249), ("bf16", 505), ("fp32", 505), ("bf16", 1018), ("fp32", 1018), ("bf16", 2024), ("bf16", 2040), ("bf16", 2042), ("fp32", 2042)]
+
+
+def first_forward_calls():
+    for dtype, d in BAND:
+        for kind in ("layer", "rms"):
+            x, _, gain, bias = _rows(1, (1 << 22) // d + 5, d, DT[dtype], d)
+            y, mean, rstd = pe.pe_norm_forward(x, gain, bias, kind=kind, eps=EPS)
+            ry, rm, rr, y_off, m_off, r_off = forward(x.double(), gain, bias, kind, EPS)
+            assert_within("y", y, ry, y_off, half_step(DT[dtype]))
+            assert_within("rstd", rstd, rr, r_off)
+            if mean is not None:
+                assert_within("mean", mean, rm, m_off)
+
+
+def test_shared_memory_just_below_48_kilobytes():
+    """In a process of its own, since a kernel that has been allowed more keeps that."""
+    import os
+    import subprocess
+    import sys
+    tests = os.path.dirname(os.path.abspath(__file__))
+    code = f"import sys; sys.path[:0] = [{os.path.dirname(tests)!r}, {tests!r}]; import test_gpu_norm_wide as t; t.first_forward_calls()"
+    alone = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert alone.returncode == 0, alone.stderr[-2000:]
