@@ -107,6 +107,7 @@ __device__ __forceinline__ void norm_load_param(const float* p, int col, bool wi
 // group: over the lanes by exchanges, over several warps by way of shared memory; `turn` alternates between two slots so that one
 // barrier per sum is enough.  Every thread of the block calls these (groups without a row too), so barriers always meet.
 constexpr int NORM_MAX_WARPS = 32;
+constexpr int NORM_WIDE_GROUPS = 8;              // groups of at least 64 threads in a block of at most 512
 template <int N>
 __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, int thread_in_group, float* slots, int& turn) {
 #pragma unroll
@@ -122,7 +123,7 @@ __device__ __forceinline__ void norm_group_sum(float (&v)[N], int G, int group, 
 #pragma unroll
       for (int k = 0; k < N; ++k) slot[(first + (thread_in_group >> 5)) * N + k] = v[k];
     }
-    sm100::named_bar_sync(1 + group, G);      // (at most four groups of more than a warp)
+    sm100::named_bar_sync(1 + group, G);      // (at most NORM_WIDE_GROUPS groups of more than a warp)
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = 0.f;
     for (int w = 0; w < warps; ++w) {
@@ -165,7 +166,7 @@ __device__ __forceinline__ void norm_rows_sum(float (&v)[N], int G, int group, i
     const int warps = G >> 5, first = group * warps;
     float* slot = slots + turn * ((int)(blockDim.x >> 5) * N);
     if ((lane & ((1 << SHIFT) - 1)) == 0) slot[(first + (thread_in_group >> 5)) * N + (lane >> SHIFT)] = a[0];
-    sm100::named_bar_sync(1 + group, G);      // (at most four groups of more than a warp)
+    sm100::named_bar_sync(1 + group, G);      // (at most NORM_WIDE_GROUPS groups of more than a warp)
     // a lane sums the warps' values (l mod N / 2) 2 and the one after it, of every 64 / N-th warp
     float2 q = make_float2(0.f, 0.f);
     for (int w = lane / (N / 2); w < warps; w += 64 / N) {
@@ -209,6 +210,7 @@ __device__ __forceinline__ void norm_sums(float (&v)[N], int G, int group, int t
 // ---------------------------------------------------------------- rows by way of shared memory
 constexpr int NORM_COLS = 8;                     // features per thread
 constexpr int NORM_MAX_THREADS = 512;
+static_assert(NORM_MAX_THREADS / 64 <= NORM_WIDE_GROUPS && 1 + NORM_WIDE_GROUPS <= 16, "a named barrier for every group");
 constexpr int NORM_STAGES = 3;
 template <typename T> __host__ __device__ constexpr int norm_rows() { return sizeof(T) == 2 ? 4 : 2; }      // R: a slot of 256 threads is 32 KB
 enum : int { NORM_WAIT_ROWS = 201, NORM_WAIT_SUMS = 202 };
@@ -426,7 +428,8 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
   griddep_wait();
   const long long workers = (long long)gridDim.x * groups, me = (long long)blockIdx.x * groups + group;
   const long long r0 = rows * me / workers, r1 = rows * (me + 1) / workers;
-  const int turns = (int)((rows + workers * R - 1) / (workers * R)), n_rows = (int)(r1 - r0);
+  const int turns = (int)((rows + workers * R - 1) / (workers * R));
+  int n_rows = (int)(r1 - r0);
   __syncthreads();
   auto issue = [&](int b) {
     const int row = b * R;
@@ -520,12 +523,13 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
     }
     norm_sums<R>(q, G, group, t, slots, turn, NormRstd{inv_d, eps});
     __syncwarp();
-    const bool lost = *(volatile int*)&abort_flag != 0;      // a thread of the group (or block) has given up: these sums, or later ones, are of rows that are not there
+    // a thread of the group (or block) has given up: these sums, or later ones, are of rows that are not there, and no more rows count
+    if (*(volatile int*)&abort_flag) n_rows = min(n_rows, row0);
     if (t == 0) {
       if (waits) issue(b + S - 1);      // every thread of the group has left the slot before this one
 #pragma unroll
       for (int k = 0; k < R; ++k)
-        if (row0 + k < n_rows && !lost) {
+        if (row0 + k < n_rows) {
           if (!RMS && mean) mean[r0 + row0 + k] = mu[k];
           if (rstd) rstd[r0 + row0 + k] = q[k];
         }
@@ -544,7 +548,7 @@ norm_forward_ring_kernel(const T* __restrict__ x, const float* __restrict__ gain
       for (int i = 0; i < NV; ++i)
         if (E == 8 || (i * G + t) * E < d) NormVec<T, E>::store(reinterpret_cast<T*>(out + (k * row_bytes + (uint32_t)(i * G) * (uint32_t)(E * sizeof(T)))), o[i]);
     };
-    if (active && !lost) {
+    if (active) {
       if (row0 + R <= n_rows) {
 #pragma unroll
         for (int k = 0; k < R; ++k) write_row(k);
@@ -706,7 +710,7 @@ struct NormEnds {
 //
 // A worker's rows come through a ring in shared memory, NORM_STAGES slots of R rows, filled by bulk copies that the group's first thread issues two slots
 // ahead: 128 KB in flight on an SM without a register spent on them, whatever the rows' alignment.  (With the next row's loads in registers,
-// 264 MB of bf16 rows of 2048 features took 1467 us, a third of the copy rate: too little in flight.)  One barrier serves the sums of R rows, and tells that the slot
+// a tensor of 1074 MB, bf16 rows of 2048 features, took 1467 us, a third of the copy rate: too little in flight.)  One barrier serves the sums of R rows, and tells that the slot
 // before has been read.  Arithmetic is on pairs of features, one instruction for both; with c = x - mu,
 //     mean(w xh) = r mean(w c),   dx = w r + c (-r^3 mean(w c)) - r mean(w),   G += (dy r) c.
 // SHORT: many examples end, and the sums over them stay in registers; otherwise they are kept beside the heads in the workspace (L2), which costs
