@@ -146,7 +146,7 @@ static BackwardPlan plan_backward(long long rows, int d, int kinds, int sm_count
       p.slabs = (d + NORM_COLS * p.G - 1) / (NORM_COLS * p.G);
     }
   }
-  // A block of 512 threads to an SM leaves half as many elements to join as two of 256 (512 x 16 x 1536, 45 us and 36; 2048 features, 268 M values, 571 and 557); rows of
+  // A block of 512 threads to an SM leaves half as many elements to join as two of 256 (512 x 16 x 1536, 45 us and 36; 2048 features, 537 M values, 571 and 557); rows of
   // fewer than 64 threads would need more shared memory than there is.
   p.groups = std::max(1, (p.mode == NORM_WHOLE && p.G >= 64 ? NORM_MAX_THREADS : 256) / p.G);
   p.kept = p.mode == NORM_CLUSTER || (p.mode == NORM_WHOLE && p.G >= 64);
