@@ -204,7 +204,8 @@ static pe_status_t launch_backward(DeviceInfo* di, const T* x, const T* dy, T* d
   const int threads = p.G * p.groups;
   // the ring, in the same place later the workers' elements, and the barriers
   const size_t slot = norm_slot_bytes(norm_rows<T>(), p.mode == NORM_WHOLE ? a.d : p.G * NORM_COLS, sizeof(T), p.mode == NORM_WHOLE);
-  const int smem = (int)(norm_bars_at(p.groups * NORM_STAGES * 2 * slot, threads, KINDS) + (size_t)p.groups * NORM_STAGES * 8);
+  a.bars_at = (uint32_t)std::max((size_t)p.groups * NORM_STAGES * 2 * slot, (size_t)threads * NORM_PARTS * KINDS * NORM_COLS * sizeof(float));
+  const int smem = (int)a.bars_at + p.groups * NORM_STAGES * 8;
   a.G = p.G;
   a.parts = reinterpret_cast<float*>(ws);
   a.ends = reinterpret_cast<int*>(ws + p.ends_at);

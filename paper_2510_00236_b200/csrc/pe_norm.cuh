@@ -220,14 +220,6 @@ __host__ __device__ constexpr size_t norm_slot_bytes(int R, int cols, int elem, 
   return whole ? (((size_t)R * cols * elem + 15) / 16 * 16 + 32) : (size_t)R * (((size_t)cols * elem + 15) / 16 * 16 + 32);
 }
 
-// Where the barriers of the backward pass are: behind the ring, and behind the workers' elements that take its place.  (Memory of a barrier is nobody else's, even after its
-// last phase: elements that were written over barriers were lost now and then.)
-enum : int { NORM_PARTS = 4 };
-__host__ __device__ constexpr size_t norm_bars_at(size_t ring_bytes, int threads, int kinds) {
-  const size_t elements = (size_t)threads * NORM_PARTS * kinds * NORM_COLS * sizeof(float);
-  return ring_bytes > elements ? ring_bytes : elements;
-}
-
 // Copies n bytes from global memory at `src` to shared memory at dst + (src & 15), dst 16-byte aligned: the 16-byte aligned part by a bulk copy
 // counted on `bar`, whose bytes are returned; begin, end: the tensor.  Only where an aligned word reaches out of the tensor its bytes are copied one element at a time.
 template <typename T>
@@ -618,7 +610,7 @@ norm_forward_wide_kernel(const T* __restrict__ x, const float* __restrict__ gain
 //     the examples that lie wholly inside, `tail`, the sum after the last end.
 // (L without an end, R): head = L.head + R.head, the rest R's.  (L with an end, R without): tail = L.tail + R.head.  Both with:
 // the example L.tail + R.head is complete and goes into tot.  No atomics: the sums' order is fixed by the launch's shape.
-enum : int { NORM_HEAD = 0, NORM_TOT = 1, NORM_STAT = 2, NORM_TAIL = 3 };      // (NORM_PARTS of them)
+enum : int { NORM_HEAD = 0, NORM_TOT = 1, NORM_STAT = 2, NORM_TAIL = 3, NORM_PARTS = 4 };
 enum : int { NORM_END = 1, NORM_LOST = 2 };
 __device__ __forceinline__ float norm_phi(int phi, float g) {
   return phi == 1 ? g * g : phi == 2 ? (float)((g > 0.f) - (g < 0.f)) : g;
@@ -646,6 +638,7 @@ struct NormBackward {
   long long rows;                       // rows of the tensors
   int B, T, d, phi, G;                  // G threads per row
   int wide;                             // gain is 16-byte aligned
+  uint32_t bars_at;                     // bytes of shared memory before the ring's barriers
   float* sums[4];                       // gain_sum, gain_stat, bias_sum, bias_stat, or NULL
   int accumulate;
   int cluster;                          // NORM_CLUSTER: blocks of a cluster
@@ -736,9 +729,10 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
   const int blocks = MODE == NORM_CLUSTER ? (int)gridDim.x / p.cluster : MODE == NORM_SLAB ? (int)gridDim.y : (int)gridDim.x;
   const int col0 = rank * G * NORM_COLS, cols = WHOLE ? d : max(0, min(d - col0, G * NORM_COLS));
   const size_t slot = norm_slot_bytes(R, WHOLE ? d : G * NORM_COLS, sizeof(T), WHOLE);
-  // [group][stage][x, dy], later the workers' elements in the same place; behind both a barrier per group and stage
+  // [group][stage][x, dy], later the workers' elements in the same place; behind both (p.bars_at) a barrier per group and stage.  (Memory of a barrier is nobody
+  // else's, even after its last phase: elements that were written over barriers were lost now and then.)
   uint8_t* ring = smem + (size_t)group * S * 2 * slot;
-  const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + (uint32_t)norm_bars_at(groups * S * 2 * slot, threads, KINDS) + group * S * 8;
+  const uint32_t ring_s = smem_u32(ring), bars = smem_u32(smem) + p.bars_at + group * S * 8;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     if (MODE == NORM_CLUSTER)
