@@ -404,7 +404,8 @@ pe_status_t microsignsgd_step(float* theta, void* theta_lp, float* m, const floa
  * is the update for whole matrices beside them.)  G = 0 gives 0; an infinity or NaN gives NaN in that matrix alone.
  * G, out: bf16 [count, rows, cols], 16-byte aligned; out may be G.  count >= 0, rows, cols >= 1 (at most 2^30), count < 65536, count * rows * cols
  * < 2^36, 1 <= steps <= 100.  Products are formed on the tensor cores from operands held as two IEEE halves (22 bits) and added up in fp32:
- * out is as close to the exact polynomial as with fp32 products (about 2e-6 relative to ||out||_F for matrices of Gaussian entries).
+ * out is as close to the exact polynomial as with fp32 products (1e-6 to 7e-6 relative to ||out||_F for matrices of Gaussian entries with and without a few
+ * directions that stand out; fp32 products 1e-6 to 5e-6).
  * workspace: device memory, 256-byte aligned, pe_orthogonalize_workspace_bytes() bytes (about 8 bytes per entry of G and 8 to 12 per entry of A, and up to 20 MB of partial products),
  * contents undefined afterwards.  Results repeat bit for bit.  After PE_ERR_TIMEOUT (see pe_get_async_status) out is as it was, but for tiles of the last
  * product that were written before its own wait ran out.

@@ -24,8 +24,8 @@ static long long ns_units(int rows, int cols, int nt, bool symmetric) {
   for (long long i = 0; i < tiles_m; ++i) units += tiles_n - i * (256 / nt);
   return units;
 }
-// Times in microseconds: a stage of 64 (12 instructions of 256 x NT x 16), what a tile costs beside its stages (set-up, the first stage's way from
-// memory, write-out), and what joining slices costs.
+// Times in microseconds, fitted to whole launches of some shapes (a stage of 256 x 128 among many takes 0.61): a stage of 64 (12 instructions of 256 x NT x 16), what a
+// tile costs beside its stages (set-up, the first stage's way from memory, write-out), and what joining slices costs.
 static NsPlan plan_product(int rows, int cols, int k, int count, bool symmetric) {
   const int stages = (k + NS_BK - 1) / NS_BK;
   NsPlan best = {128, 1, 0, 0.0};
@@ -75,7 +75,7 @@ static NsLayout ns_layout(int count, int rows, int cols) {
   // Two steps at a time where X is much longer than A: with Q = a I + b A + c A A, the next step's A is Q A Q and its polynomial another of A, so that X itself
   // is multiplied once, by Q' Q, and not twice, and X X^T formed once: five products of n^3 for two more passes over X.  Not more steps than two: what rounding leaves in
   // the directions of small singular values is multiplied by the square of the slope, up to 12 a step, in A, and by the slope, up to 3.4, in X; after two steps
-  // the errors of either way are those of fp32 products (2 to 6e-6), after three A is no longer positive and the iteration diverges.
+  // the errors of either way are those of fp32 products (2 to 7e-6 and 2 to 5e-6 for the same matrices), after three A is no longer positive and the iteration diverges.
   // 8192 x 2048: 1057 us a call against 1526; 6 x 2048 x 512: 283 and 345; 512 x 32768: 496 and 706.  (Below 256 rows the launches are what counts, and there are more.)
   l.pairs = l.n >= 256 && 3.0 * l.poly.us < 0.95 * (l.gram.us + l.apply.us);
   l.t = part(l.pairs ? 4ull * count * l.n * l.ld_n : 0);
