@@ -60,8 +60,8 @@ template <typename T, int E, bool RMS>
 static pe_status_t launch_forward(DeviceInfo* di, const T* x, const float* gain, const float* bias, long long rows, int d, float eps, T* y,
                                   float* mean, float* rstd, cudaStream_t st) {
   const int wide = aligned(gain, 16) && aligned(bias, 16), ring_G = row_threads(d);
-  // The ring where gain and bias out of L1 would hold rows up (16-bit rows of 1024 features or more: 256 x 1024 x 2048, 389 us against 563; 64 x 256 x 512, 11.4 and
-  // 11.2) or single features would (256 x 256 x 333, 49 and 128); fp32 rows go faster without (64 x 256 x 1024, 26.7 and 23.6), and so do few rows
+  // The ring where gain and bias out of L1 would hold rows up (16-bit rows of 1024 features or more: 256 x 1024 x 2048, 400 us against 563; 64 x 256 x 512, 11.4 and
+  // 11.2) or single features would (256 x 256 x 333, 52 and 128); fp32 rows go faster without (64 x 256 x 1024, 26.7 and 23.6), and so do few rows
   // (8 x 256 x 1024, 7.0 and 5.8).
   if constexpr (E == 1 || sizeof(T) == 2) {
     if (ring_G <= NORM_MAX_THREADS && rows * d >= (1ll << 22) && (E == 1 || d >= 1024)) {
