@@ -1036,7 +1036,7 @@ norm_backward_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __res
     }
     __syncwarp();
     // every thread of the group has left the slot before this one
-    if (issues && (WHOLE ? waits : __all_sync(0xffffffffu, waits))) issue(b + S - 1);      // (a slot whose wait gave up is not filled again)
+    if (issues && (WHOLE ? waits : __all_sync(0xffffffffu, waits))) issue(b + S - 1);      // (a slot whose wait gave up is not filled again: its barrier's phase is open, and must not be arrived at)
     auto write_row = [&](int k) {
       float k0 = 0.f, k1;
       if constexpr (SUMMED) {
